@@ -368,6 +368,176 @@ int sp_probe_measure_read(const void* buf, size_t bytes, int32_t reps, void* sin
  * (iters < 1, NULL pointers), SP_ERR_NO_DEVICE, SP_ERR_HIP. */
 int sp_probe_measure_mfma(int32_t iters, void* sink, float* tflops, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Operators on the head's paged cache: what a server does to it beside the
+ * classification forward.  They take no handle, allocate nothing, enqueue one
+ * or two kernels on `stream` and can be captured into a HIP graph; every
+ * check that the host can make runs before anything is enqueued.
+ * ---------------------------------------------------------------------- */
+
+/* 8-bit storage of a cache (sp_kv_store.dtype, beside SP_F32 and SP_BF16): E4M3
+ * values (4 exponent bits, 3 mantissa bits, no infinities, largest 448) with one
+ * power of two per token and KV head, for keys and for values.  A stored value v
+ * with exponent byte b (1..254) stands for v * 2^(b - 127).  b belongs to the smallest
+ * power of two that brings the row's largest finite magnitude within 448 (b = 1 at
+ * least), and v is the row's value over that power, rounded to the nearest E4M3
+ * value, ties to even; the division is exact, so v is one rounding of the value.
+ * NaN and infinities are stored as NaN. */
+enum { SP_E4M3 = 2 };
+
+/* A paged cache of any storage type, written by sp_probe_cache_write and read by
+ * sp_probe_cache_read and sp_probe_tree_attention; of SP_F32 and SP_BF16 also by the
+ * forwards (its kv member is what they take).  Layout and alignment are those of
+ * sp_kv_cache with x = 16 / sizeof(element): 4, 8 or, for SP_E4M3, 16. */
+typedef struct sp_kv_store {
+  sp_kv_cache kv;
+  int32_t dtype;               /* SP_F32, SP_BF16 or SP_E4M3 */
+  int32_t n_kv_heads;
+  int32_t head_dim;            /* 64 or 128 */
+  int32_t reserved;            /* 0 */
+  uint8_t* k_exponents;        /* device, SP_E4M3 only (else NULL): the exponent byte of slot t */
+  uint8_t* v_exponents;        /* of block p and KV head g at [p * stride_block + g * stride_head + t]; */
+  int64_t exponent_stride_block, exponent_stride_head;  /* 16-byte aligned, strides multiples of 16 */
+} sp_kv_store;
+
+/* Rows of per-head vectors: row i's head h starts at data + i * stride_row +
+ * h * stride_head (strides in elements), its head_dim values lie side by side.
+ * Any strides, so a slice of packed projections needs no copy; data aligned to its
+ * element.  16-byte aligned rows and heads are read and written 16 bytes at a time. */
+typedef struct sp_rows {
+  void* data;                  /* device */
+  int64_t stride_row, stride_head;
+  int32_t n_heads;
+  int32_t reserved;            /* 0 */
+} sp_rows;
+
+typedef enum sp_rotary_layout {
+  SP_ROTARY_HALF = 0,          /* pair p is (p, p + rotary_dim / 2), as the forwards rotate */
+  SP_ROTARY_INTERLEAVED = 1    /* pair p is (2 p, 2 p + 1) */
+} sp_rotary_layout;
+
+typedef enum sp_rotary_scaling {
+  SP_ROTARY_PLAIN = 0,   /* theta_p = base^(-2 p / rotary_dim) */
+  SP_ROTARY_LINEAR = 1,  /* theta_p / factor */
+  SP_ROTARY_NTK = 2,     /* base * factor^(rotary_dim / (rotary_dim - 2)) for base */
+  SP_ROTARY_YARN = 3,    /* YaRN's interpolation by parts: with r = original_positions theta_p / 2 pi and
+                            g = clamp((r - beta_slow) / (beta_fast - beta_slow), 0, 1),
+                            (1 - g) theta_p / factor + g theta_p; the rotated values are multiplied by
+                            attn_factor, 0.1 ln(factor) + 1 where that is 0 */
+  SP_ROTARY_CUSTOM = 4   /* theta_p = frequencies[p] (radians per position, finite); times attn_factor (0: 1) */
+} sp_rotary_scaling;
+
+typedef struct sp_rotary_config {
+  int32_t head_dim;            /* 64 or 128 */
+  int32_t rotary_dim;          /* even, 2..head_dim: the first rotary_dim values of a head turn, the rest stay */
+  int32_t layout, scaling;
+  double base;                 /* > 0 (not CUSTOM) */
+  double factor;               /* >= 1 (LINEAR, NTK, YARN) */
+  double original_positions;   /* > 0 (YARN) */
+  double beta_fast, beta_slow; /* YARN: beta_fast > beta_slow >= 0; both 0: 32 and 1 */
+  double attn_factor;          /* >= 0 (YARN, CUSTOM) */
+  const double* frequencies;   /* host, rotary_dim / 2 values (CUSTOM) */
+} sp_rotary_config;
+
+/* The rotation as the kernels take it: made once by sp_probe_rotary_init on the
+ * host, plain data that may be copied. */
+typedef struct sp_rotary {
+  int32_t head_dim, rotary_dim, layout;
+  float scale;                 /* factor on the rotated values */
+  double turns[64];            /* theta_p / 2 pi */
+} sp_rotary;
+
+/* Fill *out (host only).  SP_ERR_INVALID_ARG, SP_ERR_UNSUPPORTED (head_dim). */
+int sp_probe_rotary_init(const sp_rotary_config* cfg, sp_rotary* out);
+
+/* Rotate n_rows rows of q heads and, where k is not NULL, of k heads: head (x0, x1)
+ * of a pair at angle a = positions[i] * theta becomes
+ *   scale * (x0 cos a - x1 sin a, x1 cos a + x0 sin a),
+ * values past rotary_dim are copied.  transpose != 0: by -a, which with the same
+ * scale is the gradient with respect to the input given the output's.
+ *   dtype      SP_F32 or SP_BF16, of input and output (fp32 arithmetic, angles in fp64)
+ *   positions  device int32[n_rows]; a row at a negative position is not written
+ *   q_out, k_out  the same heads; each is its input (in place) or does not overlap it.
+ *              Two heads of an output that overlap are the caller's mistake. */
+int sp_probe_rotary(const sp_rotary* rot, int32_t dtype, int32_t transpose, int32_t n_rows,
+                    const int32_t* positions, const sp_rows* q, const sp_rows* q_out, const sp_rows* k,
+                    const sp_rows* k_out, void* stream);
+
+/* Write n_rows rows of keys and values into the cache (whose const pointers of
+ * store->kv are written here).  Row i takes row src_rows[i] of k and v (row i where
+ * src_rows is NULL) to token positions[i] of sequence seq_ids[i]; with rot (nullable) the
+ * key is rotated at that position first, in fp32.
+ *   dtype      SP_F32 or SP_BF16, of k and v; any storage type takes either
+ *   src_rows   device int32[n_rows] or NULL; n_src: rows that k and v have
+ * A row is skipped, and nothing of it written, whose position is negative or past the
+ * block table's row, whose sequence is not in [0, batch), whose source row is not in
+ * [0, n_src), or whose block id is not in [0, num_blocks).  The slots of one call must
+ * differ: two rows for one slot leave it undefined.  k and v must not overlap the cache. */
+int sp_probe_cache_write(const sp_kv_store* store, const int32_t* block_table, int32_t dtype, int32_t n_rows,
+                         const int32_t* seq_ids, const int32_t* positions, const int32_t* src_rows, int32_t n_src,
+                         const sp_rows* k, const sp_rows* v, const sp_rotary* rot, void* stream);
+
+/* Read n_rows tokens back: row i of k and v (either may be NULL) receives what token
+ * positions[i] of sequence seq_ids[i] stands for, rounded to dtype (SP_F32: exact, but
+ * for 8-bit values below 2^-126, which may become 0).  Rows that a write would skip are
+ * left as they are.  A token may be read by several rows. */
+int sp_probe_cache_read(const sp_kv_store* store, const int32_t* block_table, int32_t dtype, int32_t n_rows,
+                        const int32_t* seq_ids, const int32_t* positions, const sp_rows* k, const sp_rows* v,
+                        void* stream);
+
+/* Attention of a tree of drafted tokens (the nodes) over a sequence's cached tokens
+ * and the tree itself, as drafting with the head and verifying its drafts do it. */
+typedef struct sp_tree_config {
+  int32_t n_q_heads, n_kv_heads;  /* n_q_heads % n_kv_heads == 0, query head h reads KV head h / (n_q_heads / n_kv_heads) */
+  int32_t head_dim;               /* 64 or 128 */
+  int32_t dtype;                  /* SP_F32 (with an SP_F32 cache) or SP_BF16 (SP_BF16 or SP_E4M3): q, k, v and out */
+  int32_t kv_dtype;               /* storage of the cache */
+  int32_t max_nodes;              /* 1..256 */
+  int32_t max_batch;
+  int32_t max_seq_len;            /* longest context a call may pass; lengths are clamped to [0, max_seq_len] */
+  float scale;                    /* factor on the scores; 0: 1 / sqrt(head_dim) */
+  int32_t reserved;               /* 0 */
+} sp_tree_config;
+
+/* One call's tree: batch sequences (store->kv.batch) of n_nodes rows each, row
+ * b * n_nodes + i is node i of sequence b. */
+typedef struct sp_tree {
+  int32_t n_nodes;                /* 1..max_nodes; 1 with no mask is plain single-token decoding */
+  int32_t mask_words;             /* words per node of mask, >= ceil(n_nodes / 32) */
+  const int32_t* counts;          /* device [B] or NULL: sequence b has counts[b] nodes (clamped to
+                                     [0, n_nodes]); rows past them are neither read as keys nor written */
+  const uint32_t* mask;           /* device or NULL: node i sees node 32 w + j where bit j of
+                                     mask[b * mask_stride + i * mask_words + w] is set; bits past counts[b] mean
+                                     nothing.  Only its bits make node i see a node, itself included.
+                                     NULL: a chain, node i sees nodes 0..i */
+  int64_t mask_stride;            /* words between sequences' masks; 0: one mask for all */
+  sp_rows q, k, v;                /* q has n_q_heads heads, k and v n_kv_heads; rotated where the cache's keys are */
+  sp_rows out;                    /* n_q_heads heads; overlaps none of q, k, v */
+  float* lse;                     /* device [B * n_nodes][n_q_heads] or NULL: ln of the sum of exp(score), -inf of an empty row */
+} sp_tree;
+
+/* Every node sees all of its sequence's cached tokens [0, seq_lens[b]) and the nodes
+ * that the mask shows it; out[i] = sum_t softmax_t(scale q_i . k_t) v_t.  A node that sees
+ * nothing at all (no cached token, no node) gives 0.  What a node does not see does not
+ * reach it, whatever it holds (NaN and infinities in masked nodes' keys and values, in
+ * slots past a sequence's end).  The drafted keys and values are read from k and v and
+ * never enter the cache (sp_probe_cache_write puts the accepted ones there).
+ * Arithmetic: SP_BF16: bf16 products of the stored values (8-bit ones are exact in bf16),
+ * the softmax's weights rounded to bf16 for the product with the values; fp32 sums,
+ * statistics and partial results.  SP_F32: fp32 throughout.  The result depends on the lengths
+ * and shapes alone, not on the run (no atomics).
+ *   seq_lens, block_table  as sp_probe_forward; a block id outside [0, num_blocks) is
+ *              read as block 0 (no fault, that sequence's result means nothing)
+ *   workspace  device, 16-byte aligned, workspace_bytes >= sp_probe_tree_workspace_bytes(cfg),
+ *              not initialised; calls that share one must be ordered.  Captured graphs that
+ *              may run at the same time need their own
+ * SP_ERR_INVALID_ARG, SP_ERR_UNSUPPORTED, SP_ERR_CAPACITY (batch or nodes over the
+ * config's), SP_ERR_NO_DEVICE, SP_ERR_HIP. */
+size_t sp_probe_tree_workspace_bytes(const sp_tree_config* cfg);
+int sp_probe_tree_attention(const sp_tree_config* cfg, const sp_kv_store* store, const int32_t* seq_lens,
+                            const int32_t* block_table, const sp_tree* tree, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

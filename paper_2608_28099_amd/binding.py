@@ -18,10 +18,12 @@ STATUS = {0: "SP_OK", -1: "SP_ERR_INVALID_ARG", -2: "SP_ERR_UNSUPPORTED", -3: "S
           -4: "SP_ERR_OUT_OF_MEMORY", -5: "SP_ERR_HIP", -6: "SP_ERR_CAPACITY",
           -7: "SP_ERR_DEVICE_DATA", -8: "SP_ERR_RANGE", -9: "SP_ERR_INTERNAL"}
 SP_ERR_DEVICE_DATA, SP_ERR_RANGE, SP_ERR_INTERNAL = -7, -8, -9
-SP_F32, SP_BF16 = 0, 1
+SP_F32, SP_BF16, SP_E4M3 = 0, 1, 2
 SP_POOL_LAST, SP_POOL_MEAN = 0, 1
 SP_FLAG_DEBUG, SP_FLAG_PROFILE, SP_FLAG_LAST_ROW_ONLY = 1, 2, 4
 SP_TAP_QKV, SP_TAP_ATTN, SP_TAP_A, SP_TAP_Y, SP_TAP_X = 0, 1, 2, 3, 4
+SP_ROTARY_HALF, SP_ROTARY_INTERLEAVED = 0, 1
+SP_ROTARY_PLAIN, SP_ROTARY_LINEAR, SP_ROTARY_NTK, SP_ROTARY_YARN, SP_ROTARY_CUSTOM = 0, 1, 2, 3, 4
 SP_N_STAGES = 8
 STAGES = ("soft_prep", "attention", "merge", "o_proj", "post_norm", "gate_up", "down", "classifier")
 
@@ -31,7 +33,8 @@ EXPORTS = ("sp_probe_workspace_bytes", "sp_probe_init", "sp_probe_forward",
            "sp_probe_tap_bytes", "sp_probe_copy_tap", "sp_probe_check_device_error",
            "sp_probe_profile_read", "sp_probe_plan", "sp_probe_plan_recursive", "sp_probe_plan_config",
            "sp_probe_packed_bytes", "sp_probe_pack_weights", "sp_probe_measure_read", "sp_probe_measure_mfma",
-           "sp_probe_forward_noalloc")
+           "sp_probe_forward_noalloc", "sp_probe_rotary_init", "sp_probe_rotary", "sp_probe_cache_write",
+           "sp_probe_cache_read", "sp_probe_tree_workspace_bytes", "sp_probe_tree_attention")
 
 
 class sp_probe_config(ctypes.Structure):
@@ -64,6 +67,41 @@ class sp_probe_weights(ctypes.Structure):
 
 class sp_probe_fusion(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("fc_norm_hidden", "fc_norm_embed", "w_fc", "w_hidden_fuse")]
+
+
+class sp_kv_store(ctypes.Structure):
+    _fields_ = [("kv", sp_kv_cache), ("dtype", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("k_exponents", ctypes.c_void_p), ("v_exponents", ctypes.c_void_p),
+                ("exponent_stride_block", ctypes.c_int64), ("exponent_stride_head", ctypes.c_int64)]
+
+
+class sp_rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride_row", ctypes.c_int64), ("stride_head", ctypes.c_int64),
+                ("n_heads", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class sp_rotary_config(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("head_dim", "rotary_dim", "layout", "scaling")] + \
+        [(n, ctypes.c_double) for n in ("base", "factor", "original_positions", "beta_fast", "beta_slow",
+                                        "attn_factor")] + [("frequencies", ctypes.POINTER(ctypes.c_double))]
+
+
+class sp_rotary(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("head_dim", "rotary_dim", "layout")] + \
+        [("scale", ctypes.c_float), ("turns", ctypes.c_double * 64)]
+
+
+class sp_tree_config(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_q_heads", "n_kv_heads", "head_dim", "dtype", "kv_dtype",
+                                              "max_nodes", "max_batch", "max_seq_len")] + \
+        [("scale", ctypes.c_float), ("reserved", ctypes.c_int32)]
+
+
+class sp_tree(ctypes.Structure):
+    _fields_ = [("n_nodes", ctypes.c_int32), ("mask_words", ctypes.c_int32), ("counts", ctypes.c_void_p),
+                ("mask", ctypes.c_void_p), ("mask_stride", ctypes.c_int64), ("q", sp_rows), ("k", sp_rows),
+                ("v", sp_rows), ("out", sp_rows), ("lse", ctypes.c_void_p)]
 
 
 _lib = None
@@ -122,6 +160,22 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.sp_probe_measure_read.restype = ctypes.c_int
     lib.sp_probe_measure_mfma.argtypes = [ctypes.c_int32, vp, P(ctypes.c_float), vp]
     lib.sp_probe_measure_mfma.restype = ctypes.c_int
+    lib.sp_probe_rotary_init.argtypes = [P(sp_rotary_config), P(sp_rotary)]
+    lib.sp_probe_rotary_init.restype = ctypes.c_int
+    lib.sp_probe_rotary.argtypes = [P(sp_rotary), ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, vp,
+                                    P(sp_rows), P(sp_rows), P(sp_rows), P(sp_rows), vp]
+    lib.sp_probe_rotary.restype = ctypes.c_int
+    lib.sp_probe_cache_write.argtypes = [P(sp_kv_store), vp, ctypes.c_int32, ctypes.c_int32, vp, vp, vp,
+                                         ctypes.c_int32, P(sp_rows), P(sp_rows), P(sp_rotary), vp]
+    lib.sp_probe_cache_write.restype = ctypes.c_int
+    lib.sp_probe_cache_read.argtypes = [P(sp_kv_store), vp, ctypes.c_int32, ctypes.c_int32, vp, vp,
+                                        P(sp_rows), P(sp_rows), vp]
+    lib.sp_probe_cache_read.restype = ctypes.c_int
+    lib.sp_probe_tree_workspace_bytes.argtypes = [P(sp_tree_config)]
+    lib.sp_probe_tree_workspace_bytes.restype = ctypes.c_size_t
+    lib.sp_probe_tree_attention.argtypes = [P(sp_tree_config), P(sp_kv_store), vp, vp, P(sp_tree), vp,
+                                            ctypes.c_size_t, vp]
+    lib.sp_probe_tree_attention.restype = ctypes.c_int
     _lib = lib
     return lib
 

@@ -1,0 +1,329 @@
+"""Operators on a speculative head's paged cache, for torch tensors.
+
+    rot = ops.make_rotary(128, scaling="yarn", factor=4.0, original_positions=32768)
+    q, k = ops.rotary(rot, positions, q, k)                     # rotate projections
+    ops.cache_write(cache, seq_ids, positions, k, v)            # put them into the cache
+    out = ops.tree_attention(cache, seq_lens, q, k, v, mask)    # a drafted tree over it
+    k, v = ops.cache_read(cache, seq_ids, positions, torch.bfloat16)
+
+Thin marshalling over the C functions of include/sp_probe.h (sp_probe_rotary,
+sp_probe_cache_write, sp_probe_cache_read, sp_probe_tree_attention), which document the
+operations.  Calls go to the given stream (a raw handle; default: the current
+stream of the tensors' device) and return without waiting.  Wrong types, shapes and
+devices raise ValueError here, what the library refuses raises binding.ProbeError.
+"""
+from __future__ import annotations
+
+import ctypes
+import math
+from typing import Optional
+
+import torch
+
+from . import binding
+from .binding import ProbeError, SP_BF16, SP_E4M3, SP_F32, SP_OK
+
+_ROW_TYPES = {torch.float32: SP_F32, torch.bfloat16: SP_BF16}
+_CACHE_TYPES = {torch.float32: SP_F32, torch.bfloat16: SP_BF16, torch.float8_e4m3fn: SP_E4M3}
+_LAYOUTS = {"half": binding.SP_ROTARY_HALF, "interleaved": binding.SP_ROTARY_INTERLEAVED}
+_SCALINGS = {"none": binding.SP_ROTARY_PLAIN, "linear": binding.SP_ROTARY_LINEAR, "ntk": binding.SP_ROTARY_NTK,
+             "yarn": binding.SP_ROTARY_YARN, "custom": binding.SP_ROTARY_CUSTOM}
+
+
+def _need(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
+class _Call:
+    """The device guard and stream of one call."""
+
+    def __init__(self, device, stream):
+        _need(device.type == "cuda", "tensors must be on the GPU")
+        self.device, self.guard = device, None
+        self.given = stream
+        if device.index is not None and device.index != torch.cuda.current_device():
+            self.guard = torch.cuda.device(device)
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+        self.stream = torch.cuda.current_stream(self.device).cuda_stream if self.given is None else self.given
+        return self
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+        return False
+
+    def hold(self, *tensors):
+        """Memory that this call made lives until the given stream is past it."""
+        if self.given is not None:
+            s = torch.cuda.ExternalStream(self.given, device=self.device)
+            for t in tensors:
+                t.record_stream(s)
+
+
+def _check(status, what):
+    if status != SP_OK:
+        raise ProbeError(status, what)
+
+
+def _rows(t, name, head_dim, dtype, device, n=None):
+    """sp_rows of a [rows, heads, head_dim] tensor, or [batch, nodes, heads, head_dim] with evenly spaced rows."""
+    _need(t.dim() >= 3 and t.shape[-1] == head_dim, f"{name} must be [rows, heads, {head_dim}]")
+    _need(t.dtype == dtype and t.device == device, f"{name} must be {dtype} on {device}")
+    _need(t.stride(-1) == 1, f"{name}: the values of a head must lie side by side")
+    if t.dim() == 4:
+        _need(t.shape[0] == 1 or t.stride(0) == t.shape[1] * t.stride(1), f"{name}: rows must be evenly spaced")
+    else:
+        _need(t.dim() == 3, f"{name} must be [rows, heads, {head_dim}]")
+    _need(n is None or t.shape[0] == n, f"{name} must have {n} rows")
+    return binding.sp_rows(t.data_ptr(), t.stride(-3), t.stride(-2), t.shape[-2], 0)
+
+
+def _ids(t, name, n, device):
+    _need(t.dtype == torch.int32 and t.device == device and t.dim() == 1 and t.shape[0] == n and t.is_contiguous(),
+          f"{name} must be {n} contiguous int32 on {device}")
+    return t.data_ptr()
+
+
+# ---------------------------------------------------------------- rotary
+
+def make_rotary(head_dim, rotary_dim=None, base=10000.0, layout="half", scaling="none", factor=1.0,
+                original_positions=0, beta_fast=0.0, beta_slow=0.0, attn_factor=0.0, frequencies=None):
+    """The rotation (a binding.sp_rotary, host data) of the first rotary_dim values of a head.
+    scaling: "none", "linear", "ntk", "yarn", or "custom" with frequencies (radians per position)."""
+    _need(layout in _LAYOUTS, f"layout must be one of {sorted(_LAYOUTS)}")
+    _need(scaling in _SCALINGS, f"scaling must be one of {sorted(_SCALINGS)}")
+    dim = head_dim if rotary_dim is None else rotary_dim
+    cfg = binding.sp_rotary_config(head_dim=head_dim, rotary_dim=dim, layout=_LAYOUTS[layout],
+                                   scaling=_SCALINGS[scaling], base=base, factor=factor,
+                                   original_positions=original_positions, beta_fast=beta_fast, beta_slow=beta_slow,
+                                   attn_factor=attn_factor)
+    if frequencies is not None:
+        f = [float(x) for x in frequencies]
+        _need(len(f) == dim // 2, f"frequencies must hold {dim // 2} values")
+        cfg.frequencies = (ctypes.c_double * len(f))(*f)
+    out = binding.sp_rotary()
+    _check(binding.load().sp_probe_rotary_init(ctypes.byref(cfg), ctypes.byref(out)), "sp_probe_rotary_init")
+    return out
+
+
+def rotary(rot, positions, q, k=None, out=None, k_out=None, transpose=False, stream=None):
+    """q [rows, heads, head_dim] (and k) rotated at positions (int32 [rows]): returns the
+    rotated q, or (q, k).  out, k_out: where to write (the inputs themselves: in place);
+    rows at negative positions are not written.  transpose: the gradient's rotation (by
+    the opposite angle, with the same factor)."""
+    hd, dev = rot.head_dim, q.device
+    _need(q.dtype in _ROW_TYPES, "q must be float32 or bfloat16")
+    n = q.shape[0]
+    with _Call(dev, stream) as call:
+        made = []
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+            made.append(out)
+        if k is not None and k_out is None:
+            k_out = torch.empty(k.shape, dtype=k.dtype, device=dev)
+            made.append(k_out)
+        _need(out.shape == q.shape and (k is None or k_out.shape == k.shape), "outputs must have their inputs' shapes")
+        args = [_rows(q, "q", hd, q.dtype, dev, n), _rows(out, "out", hd, q.dtype, dev, n), None, None]
+        if k is not None:
+            args[2:] = [_rows(k, "k", hd, q.dtype, dev, n), _rows(k_out, "k_out", hd, q.dtype, dev, n)]
+        refs = [None if a is None else ctypes.byref(a) for a in args]
+        _check(binding.load().sp_probe_rotary(ctypes.byref(rot), _ROW_TYPES[q.dtype], int(bool(transpose)), n,
+                                              _ids(positions, "positions", n, dev), *refs, call.stream),
+               "sp_probe_rotary")
+        call.hold(*made)
+    return out if k is None else (out, k_out)
+
+
+# ---------------------------------------------------------------- the paged cache
+
+class PagedCache:
+    """A paged cache: keys and values [num_blocks, n_kv_heads, block_size * head_dim] in the
+    layout of include/sp_probe.h (float32, bfloat16, or float8_e4m3fn with uint8 exponents
+    [num_blocks, n_kv_heads, block_size]).  block_table int32 [batch, blocks]; without one, storage
+    is contiguous and batch says how many sequences share the blocks evenly."""
+
+    def __init__(self, k, v, block_size, block_table=None, k_exponents=None, v_exponents=None, batch=None):
+        _need(k.dtype in _CACHE_TYPES and v.dtype == k.dtype, "k and v must both be float32, bfloat16 or float8_e4m3fn")
+        _need(k.dim() == 3 and v.shape == k.shape and v.device == k.device, "k and v must be [blocks, heads, block_size * head_dim]")
+        _need(k.stride(-1) == 1 and v.stride(-1) == 1, "a head's block must be contiguous")
+        _need(block_size > 0 and k.shape[2] % block_size == 0, "the last dimension must hold block_size * head_dim values")
+        self.k, self.v, self.block_size, self.block_table = k, v, block_size, block_table
+        self.k_exponents, self.v_exponents = k_exponents, v_exponents
+        self.num_blocks, self.n_kv_heads = k.shape[0], k.shape[1]
+        self.head_dim, self.dtype, self.device = k.shape[2] // block_size, k.dtype, k.device
+        if block_table is not None:
+            _need(block_table.dtype == torch.int32 and block_table.dim() == 2 and block_table.is_contiguous()
+                  and block_table.device == k.device, "block_table must be contiguous int32 [batch, blocks] beside k")
+            self.batch, self.max_blocks = block_table.shape
+            _need(batch is None or batch == self.batch, "batch must be the block table's")
+        else:
+            _need(batch is not None and batch > 0 and self.num_blocks >= batch, "contiguous storage needs batch")
+            self.batch, self.max_blocks = batch, self.num_blocks // batch
+        st = binding.sp_kv_store(dtype=_CACHE_TYPES[k.dtype], n_kv_heads=self.n_kv_heads, head_dim=self.head_dim)
+        st.kv = binding.sp_kv_cache(k_base=k.data_ptr(), v_base=v.data_ptr(), num_blocks=self.num_blocks,
+                                    k_stride_block=k.stride(0), k_stride_head=k.stride(1),
+                                    v_stride_block=v.stride(0), v_stride_head=v.stride(1),
+                                    block_size=block_size, max_blocks_per_seq=self.max_blocks, batch=self.batch)
+        if k.dtype == torch.float8_e4m3fn:
+            for e in (k_exponents, v_exponents):
+                _need(e is not None and e.dtype == torch.uint8 and e.device == k.device and e.stride(-1) == 1
+                      and tuple(e.shape) == (self.num_blocks, self.n_kv_heads, block_size),
+                      "float8 caches need uint8 exponents [blocks, heads, block_size]")
+            _need(k_exponents.stride() == v_exponents.stride(), "both exponents must have the same strides")
+            st.k_exponents, st.v_exponents = k_exponents.data_ptr(), v_exponents.data_ptr()
+            st.exponent_stride_block, st.exponent_stride_head = k_exponents.stride(0), k_exponents.stride(1)
+        else:
+            _need(k_exponents is None and v_exponents is None, "exponents belong to float8 caches")
+        self.c = st
+
+    @classmethod
+    def allocate(cls, dtype, num_blocks, n_kv_heads, head_dim, block_size=16, block_table=None, batch=None, device="cuda"):
+        """A zeroed cache: one pool [num_blocks, n_kv_heads, 2, block_size * head_dim]."""
+        pool = torch.zeros((num_blocks, n_kv_heads, 2, block_size * head_dim), dtype=dtype, device=device)
+        e = None
+        if dtype == torch.float8_e4m3fn:
+            e = torch.full((num_blocks, n_kv_heads, 2, block_size), 127, dtype=torch.uint8, device=device)
+        return cls(pool[:, :, 0], pool[:, :, 1], block_size, block_table, None if e is None else e[:, :, 0],
+                   None if e is None else e[:, :, 1], batch)
+
+    @classmethod
+    def from_kv(cls, kv):
+        """The cache of an inputs.KVCache (what Probe.forward reads), sharing its memory."""
+        return cls(kv.pool[:, :, 0], kv.pool[:, :, 1], kv.block_size, kv.block_table,
+                   batch=None if kv.block_table is not None else kv.seq_lens.shape[0])
+
+    def _table(self):
+        return None if self.block_table is None else self.block_table.data_ptr()
+
+
+def cache_write(cache: PagedCache, seq_ids, positions, k, v, src_rows=None, rotary=None, stream=None):
+    """Row i of k and v (row src_rows[i]; all [rows, n_kv_heads, head_dim], float32 or bfloat16)
+    becomes token positions[i] of sequence seq_ids[i]; the key is rotated there first if a
+    rotation is given.  Rows with ids or positions out of range are skipped; the slots of a
+    call must differ."""
+    dev, n = cache.device, seq_ids.shape[0]
+    _need(k.dtype in _ROW_TYPES, "k must be float32 or bfloat16")
+    _need(src_rows is not None or k.shape[0] == n, f"k must have {n} rows")
+    with _Call(dev, stream) as call:
+        kr, vr = _rows(k, "k", cache.head_dim, k.dtype, dev), _rows(v, "v", cache.head_dim, k.dtype, dev, k.shape[0])
+        _need(k.dim() == 3 and v.dim() == 3, "k and v must be [rows, heads, head_dim]")
+        _check(binding.load().sp_probe_cache_write(
+            ctypes.byref(cache.c), cache._table(), _ROW_TYPES[k.dtype], n, _ids(seq_ids, "seq_ids", n, dev),
+            _ids(positions, "positions", n, dev), None if src_rows is None else _ids(src_rows, "src_rows", n, dev),
+            k.shape[0], ctypes.byref(kr), ctypes.byref(vr), None if rotary is None else ctypes.byref(rotary),
+            call.stream), "sp_probe_cache_write")
+
+
+def cache_read(cache: PagedCache, seq_ids, positions, dtype=torch.bfloat16, k=None, v=None, stream=None):
+    """Tokens positions[i] of sequences seq_ids[i] as rows [rows, n_kv_heads, head_dim] (k, v) of
+    dtype; given k and v are written (rows with ids or positions out of range are left as
+    they are)."""
+    dev, n = cache.device, seq_ids.shape[0]
+    with _Call(dev, stream) as call:
+        made = []
+        if k is None and v is None:
+            _need(dtype in _ROW_TYPES, "dtype must be float32 or bfloat16")
+            k, v = (torch.empty((n, cache.n_kv_heads, cache.head_dim), dtype=dtype, device=dev) for _ in "kv")
+            made = [k, v]
+        t = k if k is not None else v
+        _need(t.dtype in _ROW_TYPES, "k and v must be float32 or bfloat16")
+        rows = [None if x is None else _rows(x, m, cache.head_dim, t.dtype, dev, n) for x, m in ((k, "k"), (v, "v"))]
+        _check(binding.load().sp_probe_cache_read(
+            ctypes.byref(cache.c), cache._table(), _ROW_TYPES[t.dtype], n, _ids(seq_ids, "seq_ids", n, dev),
+            _ids(positions, "positions", n, dev), *[None if r is None else ctypes.byref(r) for r in rows], call.stream),
+            "sp_probe_cache_read")
+        call.hold(*made)
+    return k, v
+
+
+# ---------------------------------------------------------------- tree attention
+
+def tree_mask(parents):
+    """The mask words (int32 [.., nodes, ceil(nodes / 32)]) of trees given by parents (integers
+    [.., nodes], -1 at a root, each before its children): a node sees itself and its ancestors."""
+    parents = torch.as_tensor(parents)
+    t = parents.shape[-1]
+    flat = parents.reshape(-1, t).cpu().tolist()
+    words = torch.zeros((len(flat), t, -(-t // 32)), dtype=torch.int64)
+    for b, row in enumerate(flat):
+        for i, at in enumerate(row):
+            _need(-1 <= at < i, "a parent comes before its children")
+            if at >= 0:
+                words[b, i] = words[b, at]
+            words[b, i, i // 32] |= 1 << (i % 32)
+    words = torch.where(words >= 1 << 31, words - (1 << 32), words).to(torch.int32)
+    return words.reshape(*parents.shape, -1).to(parents.device)
+
+
+def _tree_config(cache, n_q_heads, dtype, nodes, batch, max_seq_len, scale):
+    return binding.sp_tree_config(n_q_heads=n_q_heads, n_kv_heads=cache.n_kv_heads, head_dim=cache.head_dim,
+                                  dtype=_ROW_TYPES[dtype], kv_dtype=_CACHE_TYPES[cache.dtype], max_nodes=nodes,
+                                  max_batch=batch, max_seq_len=max_seq_len, scale=scale)
+
+
+def tree_attention(cache: PagedCache, seq_lens, q, k, v, mask=None, counts=None, max_seq_len: Optional[int] = None,
+                   scale: Optional[float] = None, out=None, lse=None, workspace=None, stream=None):
+    """Attention of the nodes q [batch, nodes, n_q_heads, head_dim] over the seq_lens (int32
+    [batch]) cached tokens of each sequence and the nodes' own keys and values k, v
+    [batch, nodes, n_kv_heads, head_dim] as mask shows them: int32 words [batch, nodes, words]
+    or [nodes, words] (tree_mask; bit j of word w of node i: it sees node 32 w + j); None: each
+    node sees those up to itself.  counts (int32 [batch]): nodes of each sequence; rows past
+    them are not written.  max_seq_len: the longest sequence, shorter bounds make better
+    plans (default: what the block table holds).  lse: float32 [batch, nodes, n_q_heads] to
+    receive ln sum exp(score).  workspace: a uint8 tensor to use instead of fresh memory."""
+    dev, hd = cache.device, cache.head_dim
+    _need(q.dim() == 4 and k.dim() == 4 and v.shape == k.shape and k.shape[:2] == q.shape[:2],
+          "q, k and v must be [batch, nodes, heads, head_dim]")
+    _need(q.dtype in _ROW_TYPES, "q must be float32 or bfloat16")
+    batch, nodes, nq = q.shape[:3]
+    _need(batch == cache.batch, f"the cache has {cache.batch} sequences")
+    _need(k.shape[2] == cache.n_kv_heads, f"the cache has {cache.n_kv_heads} KV heads")
+    if max_seq_len is None:
+        max_seq_len = min(cache.max_blocks * cache.block_size, (1 << 31) - 1)
+    _need(scale is None or (math.isfinite(scale) and scale > 0), "scale must be positive")
+    with _Call(dev, stream) as call:
+        made = []
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+            made.append(out)
+        _need(out.shape == q.shape, "out must have q's shape")
+        tree = binding.sp_tree(n_nodes=nodes)
+        tree.q, tree.out = _rows(q, "q", hd, q.dtype, dev), _rows(out, "out", hd, q.dtype, dev)
+        tree.k, tree.v = _rows(k, "k", hd, q.dtype, dev), _rows(v, "v", hd, q.dtype, dev)
+        if counts is not None:
+            tree.counts = _ids(counts, "counts", batch, dev)
+        if mask is not None:
+            _need(mask.dtype in (torch.int32, torch.uint32) and mask.device == dev and mask.is_contiguous()
+                  and mask.dim() in (2, 3) and mask.shape[-2] == nodes and (mask.dim() == 2 or mask.shape[0] == batch),
+                  "mask must be contiguous int32 words [batch, nodes, words] or [nodes, words]")
+            tree.mask, tree.mask_words = mask.data_ptr(), mask.shape[-1]
+            tree.mask_stride = 0 if mask.dim() == 2 else nodes * mask.shape[-1]
+        if lse is not None:
+            _need(lse.dtype == torch.float32 and lse.device == dev and lse.is_contiguous()
+                  and tuple(lse.shape) == (batch, nodes, nq), "lse must be contiguous float32 [batch, nodes, n_q_heads]")
+            tree.lse = lse.data_ptr()
+        cfg = _tree_config(cache, nq, q.dtype, nodes, max(batch, 1), max_seq_len, scale or 0.0)
+        lib = binding.load()
+        if workspace is None:
+            n = lib.sp_probe_tree_workspace_bytes(ctypes.byref(cfg))
+            workspace = torch.empty(max(n, 16), dtype=torch.uint8, device=dev)
+            made.append(workspace)
+        _need(workspace.dtype == torch.uint8 and workspace.device == dev and workspace.is_contiguous(),
+              f"workspace must be contiguous uint8 on {dev}")
+        _check(lib.sp_probe_tree_attention(ctypes.byref(cfg), ctypes.byref(cache.c),
+                                           _ids(seq_lens, "seq_lens", batch, dev), cache._table(), ctypes.byref(tree),
+                                           workspace.data_ptr(), workspace.numel(), call.stream),
+               "sp_probe_tree_attention")
+        call.hold(*made)
+    return out
+
+
+def tree_workspace_bytes(cache: PagedCache, n_q_heads, dtype, nodes, batch=None, max_seq_len=None):
+    """Bytes of workspace that tree_attention needs for calls of these sizes (0: not supported)."""
+    cfg = _tree_config(cache, n_q_heads, dtype, nodes, cache.batch if batch is None else batch,
+                       cache.max_blocks * cache.block_size if max_seq_len is None else max_seq_len, 0.0)
+    return binding.load().sp_probe_tree_workspace_bytes(ctypes.byref(cfg))
