@@ -62,7 +62,12 @@ struct TreeParams {
   float* lse;                    // nullable
   int nodes, group, max_seq_len;
   float scale_log2;              // the scores' factor times log2(e)
+  // the plan: query rows in n_qgroups groups of n_tiles tiles of 16 (r_alloc rows in all), one
+  // workgroup of `waves` waves each; splits of split_len tokens, max_splits of max_seq_len
+  int n_qgroups, n_tiles, waves, r_alloc, split_len, max_splits;
+  float* o_part;                 // [B][n_kv][max_splits][r_alloc][hd], not divided by the sum
+  float2* ml_part;               // [B][n_kv][max_splits][r_alloc]: maximum (log2 units), sum
 };
-hipError_t launch_tree(const TreeParams& p, int storage, int hd, int n_cus, hipStream_t s);
+hipError_t launch_tree(const TreeParams& p, int storage, int hd, hipStream_t s);
 
 }  // namespace sp

@@ -124,6 +124,62 @@ int check_tree_config(const sp_tree_config* c) {
   return SP_OK;
 }
 
+// How a call of `nodes` nodes is laid out on num_cus compute units.  The splits follow the
+// config's max_batch, so that its workspace holds every call's partial results.
+struct TreePlan {
+  int n_qgroups, n_tiles, waves, r_alloc, split_len, max_splits;
+  size_t part_bytes;  // of O; the (m, l) pairs follow
+  size_t total;
+};
+
+size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+constexpr int kMaxTiles = 16;   // query tiles per workgroup: 4 waves of 4
+constexpr int kMinSplit = 256;  // tokens
+
+TreePlan tree_plan(const sp_tree_config& c, int nodes, int num_cus) {
+  TreePlan p{};
+  const int rows = nodes * (c.n_q_heads / c.n_kv_heads), tiles = (rows + 15) / 16;
+  p.n_qgroups = (tiles + kMaxTiles - 1) / kMaxTiles;
+  p.n_tiles = (tiles + p.n_qgroups - 1) / p.n_qgroups;
+  p.waves = p.n_tiles < 4 ? p.n_tiles : 4;
+  p.r_alloc = p.n_qgroups * p.n_tiles * 16;
+  p.split_len = c.max_seq_len > 64 ? (c.max_seq_len + 63) / 64 * 64 : 64;
+  p.max_splits = 1;
+  if (c.kv_dtype != SP_F32) {
+    const int64_t items = (int64_t)c.max_batch * c.n_kv_heads * p.n_qgroups;
+    const int64_t slots = (int64_t)num_cus * 3;
+    int64_t splits = (slots + items - 1) / items;
+    if (splits > 1) {
+      int64_t len = ((int64_t)c.max_seq_len + splits - 1) / splits;
+      len = (len + 63) / 64 * 64;
+      if (len < kMinSplit) len = kMinSplit;
+      if (len < p.split_len) p.split_len = (int)len;
+    }
+    p.max_splits = c.max_seq_len > 0 ? (c.max_seq_len + p.split_len - 1) / p.split_len : 1;
+  }
+  if (p.max_splits > 1) {
+    const size_t prows = (size_t)c.max_batch * c.n_kv_heads * p.max_splits * p.r_alloc;
+    p.part_bytes = align256(prows * c.head_dim * 4);
+    p.total = p.part_bytes + align256(prows * 8);
+  }
+  if (p.total < 256) p.total = 256;
+  return p;
+}
+
+// The largest plan of the calls that c allows: splits change with the number of query groups only,
+// and with that number the rows grow with the nodes.
+size_t tree_workspace(const sp_tree_config& c, int num_cus) {
+  const int group = c.n_q_heads / c.n_kv_heads;
+  size_t most = tree_plan(c, c.max_nodes, num_cus).total;
+  for (int q = 1; 16 * kMaxTiles * q / group < c.max_nodes; ++q) {  // the most nodes of q groups
+    const int nodes = 16 * kMaxTiles * q / group;
+    const size_t n = nodes > 0 ? tree_plan(c, nodes, num_cus).total : 0;
+    most = n > most ? n : most;
+  }
+  return most;
+}
+
 }  // namespace
 
 SP_API int sp_probe_rotary_init(const sp_rotary_config* c, sp_rotary* out) {
@@ -286,7 +342,9 @@ SP_API int sp_probe_cache_read(const sp_kv_store* store, const int32_t* block_ta
 
 SP_API size_t sp_probe_tree_workspace_bytes(const sp_tree_config* cfg) {
   if (check_tree_config(cfg) != SP_OK) return 0;
-  return 256;
+  int cus = 256;
+  if (current_device(&cus) != SP_OK) cus = 256;
+  return tree_workspace(*cfg, cus);
 }
 
 SP_API int sp_probe_tree_attention(const sp_tree_config* c, const sp_kv_store* store, const int32_t* seq_lens,
@@ -305,8 +363,7 @@ SP_API int sp_probe_tree_attention(const sp_tree_config* c, const sp_kv_store* s
     return SP_ERR_INVALID_ARG;
   if (store->kv.batch == 0) return SP_OK;
   if (!seq_lens || !aligned(seq_lens, 4) || !aligned(t->counts, 4) || !aligned(t->lse, 4)) return SP_ERR_INVALID_ARG;
-  if (!workspace || !aligned(workspace, 16) || workspace_bytes < sp_probe_tree_workspace_bytes(c))
-    return SP_ERR_INVALID_ARG;
+  if (!workspace || !aligned(workspace, 16)) return SP_ERR_INVALID_ARG;
   TreeParams p{};
   const int esz = size_of(c->dtype);
   bool q_vec = true, k_vec = true, v_vec = true, o_vec = true;
@@ -315,7 +372,18 @@ SP_API int sp_probe_tree_attention(const sp_tree_config* c, const sp_kv_store* s
   if ((st = check_rows(&t->v, c->n_kv_heads, esz, &v_vec)) != SP_OK) return st;
   if ((st = check_rows(&t->out, c->n_q_heads, esz, &o_vec)) != SP_OK) return st;
   int cus = 0;
-  if ((st = current_device(&cus)) != SP_OK) return st;
+  st = current_device(&cus);
+  const TreePlan pl = tree_plan(*c, t->n_nodes, st == SP_OK ? cus : 256);
+  if (workspace_bytes < pl.total) return SP_ERR_INVALID_ARG;
+  if (st != SP_OK) return st;
+  p.n_qgroups = pl.n_qgroups;
+  p.n_tiles = pl.n_tiles;
+  p.waves = pl.waves;
+  p.r_alloc = pl.r_alloc;
+  p.split_len = pl.split_len;
+  p.max_splits = pl.max_splits;
+  p.o_part = (float*)workspace;
+  p.ml_part = (float2*)((char*)workspace + pl.part_bytes);
   p.st = store_arg(store, block_table);
   p.seq_lens = seq_lens;
   p.counts = t->counts;
@@ -335,5 +403,5 @@ SP_API int sp_probe_tree_attention(const sp_tree_config* c, const sp_kv_store* s
   p.max_seq_len = c->max_seq_len;
   const double scale = c->scale > 0.f ? (double)c->scale : 1.0 / std::sqrt((double)c->head_dim);
   p.scale_log2 = (float)(scale * 1.4426950408889634);
-  return launch_tree(p, c->kv_dtype, c->head_dim, cus, (hipStream_t)stream) == hipSuccess ? SP_OK : SP_ERR_HIP;
+  return launch_tree(p, c->kv_dtype, c->head_dim, (hipStream_t)stream) == hipSuccess ? SP_OK : SP_ERR_HIP;
 }

@@ -66,41 +66,48 @@ __device__ __forceinline__ float exponent_scale(uint32_t byte) {
 }
 
 template <int HD>
-struct Rows {  // a wave's 16 query rows
+struct Rows {  // 16 query rows of a wave
   static constexpr int NC = HD / 32, NT = HD / 16;
   bf16x8 q[NC];   // Q[row li][8 (la NC + c) ..]
   f32x4 o[NT];    // O[row 4 la + r][16 nt + li]
-  float m, l;     // row li: maximum (log2 units); the lane's part of the sum
+  float m, l;     // row li: reference maximum (log2 units); the lane's part of the sum
 };
 
-// The scores s (log2 units, masked ones -inf) of the lane's NH * 4 tokens become weights;
-// m, l and o move to the new maximum.
+// A row's reference maximum moves only when a score exceeds it by more than this (log2
+// units), so weights stay below 2^8 between moves and most units skip the exchange
+// across lanes and the rescaling of O.
+constexpr float kRescaleLog2 = 8.0f;
+
+// The lane's scores s (products not yet scaled; masked ones -inf) of NH * 4 tokens become
+// weights 2^(s scale - m); where the maximum moves, l and o follow.
 template <int HD, int NH>
-__device__ __forceinline__ void softmax_step(Rows<HD>& st, f32x4 (&s)[NH], int la) {
-  float mx = st.m;
+__device__ __forceinline__ void softmax_step(Rows<HD>& st, f32x4 (&s)[NH], float scale, int la) {
+  float mx = fmaxf(s[0][0], s[0][1]);
 #pragma unroll
-  for (int h = 0; h < NH; ++h)
+  for (int i = 2; i < 4 * NH; ++i) mx = fmaxf(mx, s[i / 4][i % 4]);
+  mx *= scale;
+  if (__any(mx > st.m + kRescaleLog2)) {
+    mx = fmaxf(mx, __shfl_xor(mx, 16));
+    mx = fmaxf(mx, __shfl_xor(mx, 32));
+    mx = fmaxf(mx, st.m);
+    const float alpha = fast_exp2(st.m - mx);
+    st.m = mx;
+    st.l *= alpha;
+    float ar[4];  // the factors of this lane's O rows 4 la + r
 #pragma unroll
-    for (int r = 0; r < 4; ++r) mx = fmaxf(mx, s[h][r]);
-  mx = fmaxf(mx, __shfl_xor(mx, 16));
-  mx = fmaxf(mx, __shfl_xor(mx, 32));
-  const float alpha = fast_exp2(st.m - mx);
-  st.m = mx;
-  st.l *= alpha;
+    for (int r = 0; r < 4; ++r) ar[r] = __shfl(alpha, 4 * la + r);
+#pragma unroll
+    for (int nt = 0; nt < Rows<HD>::NT; ++nt)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) st.o[nt][r] *= ar[r];
+  }
 #pragma unroll
   for (int h = 0; h < NH; ++h)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      s[h][r] = fast_exp2(s[h][r] - mx);
+      s[h][r] = fast_exp2(fmaf(s[h][r], scale, -st.m));
       st.l += s[h][r];
     }
-  float ar[4];
-#pragma unroll
-  for (int r = 0; r < 4; ++r) ar[r] = __shfl(alpha, 4 * la + r);
-#pragma unroll
-  for (int nt = 0; nt < Rows<HD>::NT; ++nt)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) st.o[nt][r] *= ar[r];
 }
 
 // The weights of 8 tokens (scores h0 and h0 + 1) as a bf16 operand.  Rounded to nearest:
@@ -116,88 +123,165 @@ __device__ __forceinline__ bf16x8 weights8(const f32x4 (&s)[NH], int h0) {
   return w;
 }
 
-// One unit of cached tokens t0 .. (`limit` of them there are).
+// LDS image of a unit, in 16-byte pieces: NSUB runs of 16 tokens (each inside one
+// block), their keys, then their values.  A run's keys: piece c * 16 + t = 16 bytes of dims
+// of token t; its values: 8-bit: piece d = dim d of its 16 tokens; bf16: piece
+// (2 nt + e) * 16 + i = dim 16 nt + i of its tokens 8 e .. 8 e + 7.  The 4-piece pad between
+// the runs' keys lets the 16 lanes of a key fragment (4 or 8 tokens of every run) hit 16
+// different 16-byte bank groups; a value fragment is 256 bytes in a row per 16 lanes.
+// Pieces go from memory to LDS 64 at a time, each lane its own address.
 template <int HD, bool E8>
-__device__ __forceinline__ void cache_unit(const TreeParams& p, Rows<HD>& st, int b, int g, int t0, int limit, int li,
-                                           int la) {
-  constexpr int NC = HD / 32, NT = HD / 16, NH = E8 ? 4 : 2, TPL = 4 * NH, X = E8 ? 16 : 8;
-  const StoreArg& c = p.st;
-  const int64_t bs = (int64_t)1 << c.bs_log2;
-  // tokens past the end read the unit's first instead (they lie in a block the sequence owns)
-  const int gk = TPL * (li >> 2), gv = TPL * la;  // first of the lane's group of tokens, as key and as value
-  const int tk = t0 + (gk < limit ? gk : 0), tv = t0 + (gv < limit ? gv : 0);
-  const int64_t bk = block_of(c, b, tk), bv = block_of(c, b, tv);
-  const int64_t sk = tk & (bs - 1), sv = tv & (bs - 1);
-  f32x4 s[NH];
-#pragma unroll
-  for (int h = 0; h < NH; ++h) s[h] = f32x4{0.f, 0.f, 0.f, 0.f};
-  u32x4 ev = u32x4{0, 0, 0, 0};
-  if constexpr (E8) {
-    const uint8_t* kb = (const uint8_t*)c.k + bk * c.k_sb + g * c.k_sh;
-    const u32x4 ek = ld16v(c.k_exp + bk * c.e_sb + g * c.e_sh + sk);
-    ev = ld16v(c.v_exp + bv * c.e_sb + g * c.e_sh + sv);
-#pragma unroll
-    for (int h = 0; h < NH; ++h) {
-      const float scale = exponent_scale((ek[h] >> (8 * (li & 3))) & 0xffu);
-#pragma unroll
-      for (int q = 0; q < NC / 2; ++q) {
-        const u32x4 w = ld16v(kb + ((int64_t)(la * (NC / 2) + q) * bs + sk + 4 * h + (li & 3)) * X);
-        s[h] = mfma16x16x32_bf16(from_e4m3(w[0], w[1], scale), st.q[2 * q], s[h]);
-        s[h] = mfma16x16x32_bf16(from_e4m3(w[2], w[3], scale), st.q[2 * q + 1], s[h]);
-      }
-    }
-  } else {
-    const bf16* kb = (const bf16*)c.k + bk * c.k_sb + g * c.k_sh;
-#pragma unroll
-    for (int h = 0; h < NH; ++h)
-#pragma unroll
-      for (int q = 0; q < NC; ++q) {
-        const u32x4 w = ld16v(kb + ((int64_t)(la * NC + q) * bs + sk + 4 * h + (li & 3)) * X);
-        s[h] = mfma16x16x32_bf16(__builtin_bit_cast(bf16x8, w), st.q[q], s[h]);
-      }
+struct Unit {
+  static constexpr int NSUB = E8 ? 4 : 2, TOKENS = 16 * NSUB;
+  static constexpr int SUB = E8 ? HD : 2 * HD;       // pieces of a run's keys, or of its values
+  static constexpr int KP = SUB + 4, VB = NSUB * KP;
+  static constexpr int EB = VB + NSUB * SUB;         // exponents: 64 words (keys 16, values 16, twice)
+  static constexpr int PIECES = EB + (E8 ? 16 : 0);
+  static constexpr int IPG = SUB / 64;               // loads of 64 pieces per run
+  static constexpr int NI = 2 * NSUB * IPG;          // per unit
+  static __device__ __forceinline__ int group_base(int gi) { return gi < NSUB ? gi * KP : VB + (gi - NSUB) * SUB; }
+  // byte offset of piece q of a run from its first token's place in the block
+  static __device__ __forceinline__ uint32_t key_off(int q, int bs) { return (uint32_t)((q >> 4) * bs + (q & 15)) * 16u; }
+  static __device__ __forceinline__ uint32_t value_off(int q, int bs) {
+    if (E8) return (uint32_t)(q * bs);
+    return (uint32_t)((16 * (q >> 5) + (q & 15)) * bs * 2 + ((q >> 4) & 1) * 16);
   }
-#pragma unroll
-  for (int h = 0; h < NH; ++h)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) s[h][r] = TPL * la + 4 * h + r < limit ? s[h][r] * p.scale_log2 : -INFINITY;
-  softmax_step<HD, NH>(st, s, la);
-  if constexpr (E8) {
-    // the values' exponents; slots past the end may hold anything
-#pragma unroll
-    for (int h = 0; h < NH; ++h)
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-        s[h][r] = TPL * la + 4 * h + r < limit ? s[h][r] * exponent_scale((ev[h] >> (8 * r)) & 0xffu) : 0.f;
-    const bf16x8 p0 = weights8(s, 0), p1 = weights8(s, 2);
-    const uint8_t* vb = (const uint8_t*)c.v + bv * c.v_sb + g * c.v_sh + sv;
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      u32x4 w = ld16v(vb + (16 * nt + li) * bs);
-#pragma unroll
-      for (int h = 0; h < 4; ++h) {
-        const int keep = limit - (TPL * la + 4 * h);  // the word's tokens that there are
-        w[h] = keep >= 4 ? w[h] : keep > 0 ? w[h] & ((1u << (8 * keep)) - 1) : 0u;
-      }
-      st.o[nt] = mfma16x16x32_bf16(p0, from_e4m3(w[0], w[1], 1.f), st.o[nt]);
-      st.o[nt] = mfma16x16x32_bf16(p1, from_e4m3(w[2], w[3], 1.f), st.o[nt]);
-    }
+};
+
+// Physical block ids of a split: two windows of kIdWin logical blocks, window w in half w & 1.
+constexpr int kIdWin = 256;
+constexpr int kStages = 3;
+
+// Direct 4-byte loads into LDS: lane l's word lands at dst + 4 l (dst uniform).
+__device__ __forceinline__ void ld4_to_lds(const void* addr, void* dst) {
+  const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)dst;
+  asm volatile("global_load_lds_dword %0, off" : : "v"(addr), "{m0}"(lds) : "memory");
+}
+
+// Wait until at most k units of PPL loads each remain in flight (k <= K).
+template <int PPL, int K>
+__device__ __forceinline__ void wait_units_le(int k) {
+  if constexpr (K == 0) {
+    wait_vmcnt<0>();
   } else {
-    const bf16x8 p0 = weights8(s, 0);
-    const bf16* vb = (const bf16*)c.v + bv * c.v_sb + g * c.v_sh + sv;
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      u32x4 w = ld16v(vb + (16 * nt + li) * bs);
-#pragma unroll
-      for (int h = 0; h < 4; ++h) {
-        const int keep = limit - (TPL * la + 2 * h);
-        w[h] = keep >= 2 ? w[h] : keep == 1 ? w[h] & 0xffffu : 0u;
-      }
-      st.o[nt] = mfma16x16x32_bf16(p0, __builtin_bit_cast(bf16x8, w), st.o[nt]);
-    }
+    if (k >= K) wait_vmcnt<K * PPL>();
+    else wait_units_le<PPL, K - 1>(k);
   }
 }
 
-// Nodes 32 u .. of n as keys and values.  `seen`: those that row li sees.
+// Bits of a word of E bytes per value whose first token is `keep` tokens before the end.
+template <int E>
+__device__ __forceinline__ uint32_t keep_mask(int keep) {
+  return keep >= 4 / E ? ~0u : keep > 0 ? (1u << (8 * E * keep)) - 1 : 0u;
+}
+
+// One staged unit of cached tokens, `limit` of them there, for the wave's ntw tiles.
+template <int HD, bool E8, int TPW>
+__device__ __forceinline__ void cache_unit(Rows<HD> (&st)[TPW], int ntw, const u32x4* sb, int limit, float scale, int li,
+                                           int la) {
+  using L = Unit<HD, E8>;
+  constexpr int NC = HD / 32, NT = HD / 16, NH = E8 ? 4 : 2, TPL = 4 * NH;
+  const int run = TPL * (li >> 2) / 16, first = TPL * (li >> 2) % 16 + (li & 3);  // of the lane's key
+  f32x4 s[TPW][NH];
+#pragma unroll
+  for (int t = 0; t < TPW; ++t)
+#pragma unroll
+    for (int h = 0; h < NH; ++h) s[t][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+  if constexpr (E8) {
+    const u32x4 ek = sb[L::EB + run];
+#pragma unroll
+    for (int h = 0; h < NH; ++h) {
+      const float f = exponent_scale((ek[h] >> (8 * (li & 3))) & 0xffu);
+#pragma unroll
+      for (int q = 0; q < NC / 2; ++q) {
+        const u32x4 w = sb[run * L::KP + (la * (NC / 2) + q) * 16 + first + 4 * h];
+        const bf16x8 k0 = from_e4m3(w[0], w[1], f), k1 = from_e4m3(w[2], w[3], f);
+#pragma unroll
+        for (int t = 0; t < TPW; ++t)
+          if (t < ntw) {
+            s[t][h] = mfma16x16x32_bf16(k0, st[t].q[2 * q], s[t][h]);
+            s[t][h] = mfma16x16x32_bf16(k1, st[t].q[2 * q + 1], s[t][h]);
+          }
+      }
+    }
+  } else {
+    u32x4 kf[NH][NC];
+#pragma unroll
+    for (int h = 0; h < NH; ++h)
+#pragma unroll
+      for (int q = 0; q < NC; ++q) kf[h][q] = sb[run * L::KP + (la * NC + q) * 16 + first + 4 * h];
+#pragma unroll
+    for (int t = 0; t < TPW; ++t)
+      if (t < ntw)
+#pragma unroll
+        for (int q = 0; q < NC; ++q)
+#pragma unroll
+          for (int h = 0; h < NH; ++h)
+            s[t][h] = mfma16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[h][q]), st[t].q[q], s[t][h]);
+  }
+  // values are read once the scores' products are issued, into registers the keys held
+  __builtin_amdgcn_sched_barrier(0);
+  u32x4 vf[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+    vf[nt] = E8 ? sb[L::VB + la * L::SUB + 16 * nt + li]
+                : sb[L::VB + (la >> 1) * L::SUB + (2 * nt + (la & 1)) * 16 + li];
+  u32x4 ev = u32x4{0, 0, 0, 0};
+  if constexpr (E8) ev = sb[L::EB + 4 + la];
+  if (limit < L::TOKENS) {  // a tail: tokens past the end may hold anything
+    int lim = limit;
+    asm volatile("" : "+s"(lim));  // (keeps the mask a branch that whole units skip)
+#pragma unroll
+    for (int t = 0; t < TPW; ++t)
+#pragma unroll
+      for (int i = 0; i < TPL; ++i)
+        if (TPL * la + i >= lim) s[t][i / 4][i % 4] = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const uint32_t keep = E8 ? keep_mask<1>(lim - (TPL * la + 4 * w)) : keep_mask<2>(lim - (TPL * la + 2 * w));
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) vf[nt][w] &= keep;
+      ev[w] &= keep;
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < TPW; ++t)
+    if (t < ntw) {
+      softmax_step<HD, NH>(st[t], s[t], scale, la);
+      if constexpr (E8)
+#pragma unroll
+        for (int i = 0; i < TPL; ++i) s[t][i / 4][i % 4] *= exponent_scale((ev[i / 4] >> (8 * (i % 4))) & 0xffu);
+    }
+  if constexpr (E8) {
+    bf16x8 p0[TPW], p1[TPW];
+#pragma unroll
+    for (int t = 0; t < TPW; ++t) {
+      p0[t] = weights8(s[t], 0);
+      p1[t] = weights8(s[t], 2);
+    }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const bf16x8 v0 = from_e4m3(vf[nt][0], vf[nt][1], 1.f), v1 = from_e4m3(vf[nt][2], vf[nt][3], 1.f);
+#pragma unroll
+      for (int t = 0; t < TPW; ++t)
+        if (t < ntw) {
+          st[t].o[nt] = mfma16x16x32_bf16(p0[t], v0, st[t].o[nt]);
+          st[t].o[nt] = mfma16x16x32_bf16(p1[t], v1, st[t].o[nt]);
+        }
+    }
+  } else {
+#pragma unroll
+    for (int t = 0; t < TPW; ++t)
+      if (t < ntw) {
+        const bf16x8 p0 = weights8(s[t], 0);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+          st[t].o[nt] = mfma16x16x32_bf16(p0, __builtin_bit_cast(bf16x8, vf[nt]), st[t].o[nt]);
+      }
+  }
+}
+
+// Nodes 32 u .. of n as keys and values for one tile.  `seen`: those that row li sees.
 template <int HD>
 __device__ __forceinline__ void node_unit(const TreeParams& p, Rows<HD>& st, int b, int g, int u, int n, uint32_t seen,
                                           int li, int la) {
@@ -214,9 +298,9 @@ __device__ __forceinline__ void node_unit(const TreeParams& p, Rows<HD>& st, int
       s[h] = mfma16x16x32_bf16(__builtin_bit_cast(bf16x8, row8(kr + 8 * (la * NC + q), p.k_vec)), st.q[q], s[h]);
 #pragma unroll
     for (int r = 0; r < 4; ++r)
-      s[h][r] = (seen >> (8 * la + 4 * h + r)) & 1 ? s[h][r] * p.scale_log2 : -INFINITY;
+      s[h][r] = (seen >> (8 * la + 4 * h + r)) & 1 ? s[h][r] : -INFINITY;
   }
-  softmax_step<HD, 2>(st, s, la);
+  softmax_step<HD, 2>(st, s, p.scale_log2, la);
   const bf16x8 p0 = weights8(s, 0);
   bf16x8 v[NT];
   bool odd = false;  // a value that is not finite
@@ -250,48 +334,217 @@ __device__ __forceinline__ void node_unit(const TreeParams& p, Rows<HD>& st, int
   }
 }
 
-// One wave per (16 query rows, KV head, sequence).
-template <int HD, bool E8>
-__global__ __launch_bounds__(64) void tree_wave(const TreeParams p) {
-  constexpr int NC = HD / 32, NT = HD / 16, U = E8 ? 64 : 32;
-  const int lane = threadIdx.x, li = lane & 15, la = lane >> 4;
-  const int row0 = 16 * blockIdx.x, g = blockIdx.y, b = blockIdx.z;
+__device__ __forceinline__ float lse_of(float m, float l) {
+  return l > 0.f || l != l ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+}
+
+// One workgroup per (group of query tiles, KV head; split; sequence): W waves, an even
+// share of the group's tiles each (at most TPW).  The split's units pass through three LDS stages,
+// loaded two units ahead; every fragment that a wave reads from LDS serves all its tiles.
+// A sequence's last split takes the nodes too.  A sequence of one split is finished here,
+// else its splits leave (m, l) and O for tree_merge.
+template <int HD, bool E8, int W, int TPW>
+__global__ __launch_bounds__(64 * W) void tree_split(const TreeParams p) {
+  using L = Unit<HD, E8>;
+  constexpr int NC = HD / 32, NT = HD / 16, NI = L::NI, NSUB = L::NSUB, U = L::TOKENS;
+  constexpr int PPL = (NI + W - 1) / W, LOADS = PPL + (E8 ? 1 : 0), D = kStages - 1;
+  static_assert(W <= 2 * NI && D * LOADS < 64, "loads in flight");
+  __shared__ u32x4 stage[kStages][L::PIECES];
+  __shared__ int blk_ids[2][kIdWin];
+  const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, la = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  __builtin_assume(wave >= 0 && wave < W);
+  const int g = blockIdx.x % p.st.n_kv, qg = blockIdx.x / p.st.n_kv, b = blockIdx.z, s = blockIdx.y;
   const int n = count_of(p, b), rows = n * p.group;
-  if (row0 >= rows) return;
   const int len = clamp_len(p.seq_lens, b, p.max_seq_len);
-  const int row = min(row0 + li, rows - 1), node = row / p.group;
-  Rows<HD> st;
-  const bf16* q = (const bf16*)p.q.data + ((int64_t)b * p.nodes + node) * p.q.row +
-                  (int64_t)(g * p.group + row % p.group) * p.q.head;
+  const int t0 = s * p.split_len, t1 = min(len, t0 + p.split_len);
+  if ((s > 0 && t0 >= len) || qg * p.n_tiles * 16 >= rows) return;
+  const bool whole = len <= p.split_len, last = t1 == len;
+  const int tb = wave * p.n_tiles / W, ntw = TPW == 1 ? 1 : (wave + 1) * p.n_tiles / W - tb;
+  const int row0 = (qg * p.n_tiles + tb) * 16;
+
+  Rows<HD> st[TPW];
 #pragma unroll
-  for (int c = 0; c < NC; ++c) st.q[c] = __builtin_bit_cast(bf16x8, row8(q + 8 * (la * NC + c), p.q_vec));
+  for (int t = 0; t < TPW; ++t) {
+    const int row = min(row0 + 16 * t + li, rows - 1);
+    const bf16* q = (const bf16*)p.q.data + ((int64_t)b * p.nodes + row / p.group) * p.q.row +
+                    (int64_t)(g * p.group + row % p.group) * p.q.head;
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) st.o[nt] = f32x4{0.f, 0.f, 0.f, 0.f};
-  st.m = kNegBig;
-  st.l = 0.f;
-  for (int t = 0; t < len; t += U) cache_unit<HD, E8>(p, st, b, g, t, len - t, li, la);
-  for (int u = 0; 32 * u < n; ++u) node_unit<HD>(p, st, b, g, u, n, seen_word(p, b, node, u, n), li, la);
-  float l = st.l;
-  l += __shfl_xor(l, 16);
-  l += __shfl_xor(l, 32);
-  if (p.lse && la == 0 && row0 + li < rows)
-    p.lse[((int64_t)b * p.nodes + node) * (p.st.n_kv * p.group) + g * p.group + row % p.group] =
-        l > 0.f || l != l ? (st.m + log2f(l)) * 0.6931471805599453f : -INFINITY;
-  float inv[4];
+    for (int c = 0; c < NC; ++c) st[t].q[c] = __builtin_bit_cast(bf16x8, row8(q + 8 * (la * NC + c), p.q_vec));
 #pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    const float lr = __shfl(l, 4 * la + r);
-    inv[r] = lr == 0.f ? 0.f : 1.0f / lr;
+    for (int nt = 0; nt < NT; ++nt) st[t].o[nt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    st[t].m = kNegBig;
+    st[t].l = 0.f;
+  }
+
+  const int nunits = (t1 - t0 + U - 1) / U;
+  if (nunits > 0) {
+    const StoreArg& c = p.st;
+    constexpr int ESZ = E8 ? 1 : 2;
+    const char* kbase = (const char*)c.k + g * c.k_sh * ESZ;
+    const char* vbase = (const char*)c.v + g * c.v_sh * ESZ;
+    const int bs = 1 << c.bs_log2;
+    const int lb0 = t0 >> c.bs_log2, nlb = ((t1 - 1) >> c.bs_log2) - lb0 + 1;
+    const int* bt_row = c.block_table ? c.block_table + (int64_t)b * c.mbps + lb0 : nullptr;
+    if (bt_row)
+      for (int i = tid; i < min(nlb, 2 * kIdWin); i += 64 * W) blk_ids[i / kIdWin][i % kIdWin] = bt_row[i];
+    auto load_window = [&](int w) __attribute__((always_inline)) {
+      for (int j = wave; j < kIdWin / 64; j += W)  // past the end: the last id again
+        ld4_to_lds(bt_row + min(w * kIdWin + j * 64 + lane, nlb - 1), &blk_ids[w & 1][j * 64]);
+    };
+    // nothing that the compiler counts stays in flight past this point
+    wait_vmcnt<0>();
+    lds_barrier();
+    uint32_t lane_off[PPL];
+    int gsel[PPL], lds_piece[PPL];
+#pragma unroll
+    for (int j = 0; j < PPL; ++j) {
+      const int slot = (j * W + wave) % NI;  // (a wave count that does not divide NI loads a few twice)
+      gsel[j] = L::IPG % W == 0 ? j * W / L::IPG : slot / L::IPG;
+      lds_piece[j] = L::group_base(gsel[j]) + (slot % L::IPG) * 64;
+      const int q = (slot % L::IPG) * 64 + lane;
+      lane_off[j] = gsel[j] < NSUB ? L::key_off(q, bs) : L::value_off(q, bs);
+    }
+    const int er = (lane >> 2) & 3;  // exponents: lanes 0..15 the keys', 16..31 the values', then both again
+    // Loads are streaming (read once by this launch), unless another query group reads the
+    // same blocks, or a unit takes less than its 64 bytes of a dim's row of values.
+    const bool k_stream = p.n_qgroups == 1, v_stream = k_stream && bs * ESZ <= 64;
+    auto issue = [&](int u, int buf) __attribute__((always_inline)) {
+      int64_t blk[NSUB];
+      int slot[NSUB];
+#pragma unroll
+      for (int r = 0; r < NSUB; ++r) {
+        int t = t0 + U * u + 16 * r;
+        t = t < t1 ? t : t0 + U * u;  // a run past the end reads the unit's first again
+        const int rel = (t >> c.bs_log2) - lb0;
+        slot[r] = t & (bs - 1);
+        if (bt_row) blk[r] = __builtin_amdgcn_readfirstlane(blk_ids[((unsigned)rel / kIdWin) & 1][(unsigned)rel % kIdWin]);
+        else blk[r] = (int64_t)b * c.mbps + lb0 + rel;
+      }
+      const char *kr[NSUB], *vr[NSUB];
+#pragma unroll
+      for (int r = 0; r < NSUB; ++r) {
+        blk[r] = blk[r] >= 0 && blk[r] < c.num_blocks ? blk[r] : 0;
+        kr[r] = kbase + blk[r] * c.k_sb * ESZ + slot[r] * 16;
+        vr[r] = vbase + blk[r] * c.v_sb * ESZ + slot[r] * ESZ;
+      }
+#pragma unroll
+      for (int j = 0; j < PPL; ++j) {
+        const char* base = kr[0];
+#pragma unroll
+        for (int r = 1; r < NSUB; ++r) base = gsel[j] == r ? kr[r] : base;
+#pragma unroll
+        for (int r = 0; r < NSUB; ++r) base = gsel[j] == NSUB + r ? vr[r] : base;
+        if (gsel[j] < NSUB ? k_stream : v_stream) ld16_to_lds(base, lane_off[j], &stage[buf][lds_piece[j]]);
+        else ld16_to_lds<false>(base, lane_off[j], &stage[buf][lds_piece[j]]);
+      }
+      if constexpr (E8) {
+        int64_t eb = blk[0];
+        int es = slot[0];
+#pragma unroll
+        for (int r = 1; r < NSUB; ++r) {
+          eb = er == r ? blk[r] : eb;
+          es = er == r ? slot[r] : es;
+        }
+        const uint8_t* e = lane & 16 ? c.v_exp : c.k_exp;
+        ld4_to_lds(e + eb * c.e_sb + g * c.e_sh + es + 4 * (lane & 3), &stage[buf][L::EB]);
+      }
+    };
+    const int lastu = nunits - 1;
+    // entering window w when issuing unit v: window w + 1 replaces w - 1, which no later unit reads
+    auto next_window = [&](int v) __attribute__((always_inline)) {
+      const int w = (((t0 + U * v) >> c.bs_log2) - lb0) / kIdWin;
+      const int wp = (((t0 + U * (v - 1)) >> c.bs_log2) - lb0) / kIdWin;
+      if (bt_row && w != wp && (w + 1) * kIdWin < nlb) load_window(w + 1);
+    };
+#pragma unroll
+    for (int v = 0; v < D; ++v)
+      if (v <= lastu) issue(v, v);
+    int buf = 0;
+    for (int u = 0; u < nunits; ++u) {
+      // this wave's loads of unit u have landed; after the barrier everyone's have, and all are past unit u - 1
+      wait_units_le<LOADS, D - 1>(min(u + D - 1, lastu) - u);
+      lds_barrier();
+      if (u + D <= lastu) {
+        issue(u + D, buf == 0 ? kStages - 1 : buf - 1);
+        next_window(u + D);
+      }
+      cache_unit<HD, E8, TPW>(st, ntw, stage[buf], t1 - (t0 + U * u), p.scale_log2, li, la);
+      buf = buf == kStages - 1 ? 0 : buf + 1;
+    }
   }
 #pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    const int orow = row0 + 4 * la + r;
-    if (orow >= rows) continue;
-    bf16* o = (bf16*)p.out.data + ((int64_t)b * p.nodes + orow / p.group) * p.out.row +
-              (int64_t)(g * p.group + orow % p.group) * p.out.head;
+  for (int t = 0; t < TPW; ++t) {
+    const int r0 = row0 + 16 * t;
+    if (t >= ntw || r0 >= rows) continue;
+    if (last) {
+      const int node = min(r0 + li, rows - 1) / p.group;
+      for (int u = 0; 32 * u < n; ++u) node_unit<HD>(p, st[t], b, g, u, n, seen_word(p, b, node, u, n), li, la);
+    }
+    float l = st[t].l;
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (whole) {
+      const int row = r0 + li;
+      if (p.lse && la == 0 && row < rows)
+        p.lse[((int64_t)b * p.nodes + row / p.group) * (p.st.n_kv * p.group) + g * p.group + row % p.group] = lse_of(st[t].m, l);
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) o[16 * nt + li] = (bf16)(st.o[nt][r] * inv[r]);
+      for (int r = 0; r < 4; ++r) {
+        const float lr = __shfl(l, 4 * la + r);
+        const float inv = lr == 0.f ? 0.f : 1.0f / lr;
+        const int orow = r0 + 4 * la + r;
+        if (orow >= rows) continue;
+        bf16* o = (bf16*)p.out.data + ((int64_t)b * p.nodes + orow / p.group) * p.out.row +
+                  (int64_t)(g * p.group + orow % p.group) * p.out.head;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) o[16 * nt + li] = (bf16)(st[t].o[nt][r] * inv);
+      }
+    } else {
+      const int64_t prow = (((int64_t)b * p.st.n_kv + g) * p.max_splits + s) * p.r_alloc + r0;
+      if (la == 0) p.ml_part[prow + li] = make_float2(st[t].m, l);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) p.o_part[(prow + 4 * la + r) * HD + 16 * nt + li] = st[t].o[nt][r];
+    }
   }
+}
+
+// Joins the splits of the sequences that have several: one wave per query row, its lanes
+// along the dims, every split's O weighted by 2^(m - the largest m).
+template <int HD, typename T>
+__global__ __launch_bounds__(256) void tree_merge(const TreeParams p) {
+  constexpr int V = HD / 64;
+  const int lane = threadIdx.x & 63, g = blockIdx.y, b = blockIdx.z;
+  const int row = 4 * blockIdx.x + (threadIdx.x >> 6);
+  const int len = clamp_len(p.seq_lens, b, p.max_seq_len);
+  if (len <= p.split_len || row >= count_of(p, b) * p.group) return;
+  const int ns = (len + p.split_len - 1) / p.split_len;
+  const int64_t base = ((int64_t)b * p.st.n_kv + g) * p.max_splits * p.r_alloc + row;
+  float m = kNegBig;
+  for (int s = lane; s < ns; s += 64) m = fmaxf(m, p.ml_part[base + (int64_t)s * p.r_alloc].x);
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
+  float l = 0.f, acc[V] = {};
+#pragma unroll 4
+  for (int s = 0; s < ns; ++s) {
+    const int64_t at = base + (int64_t)s * p.r_alloc;
+    const float2 ml = p.ml_part[at];
+    const float w = fast_exp2(ml.x - m);
+    l += w * ml.y;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const float x = p.o_part[at * HD + V * lane + i];
+      acc[i] += w * x;
+    }
+  }
+  const int head = g * p.group + row % p.group;
+  const int64_t node = (int64_t)b * p.nodes + row / p.group;
+  if (p.lse && lane == 0) p.lse[node * (p.st.n_kv * p.group) + head] = lse_of(m, l);
+  const float inv = l == 0.f ? 0.f : 1.0f / l;
+  T* o = (T*)p.out.data + node * p.out.row + (int64_t)head * p.out.head;
+#pragma unroll
+  for (int i = 0; i < V; ++i) o[V * lane + i] = from_f32<T>(acc[i] * inv);
 }
 
 // ---------------------------------------------------------------- fp32
@@ -418,21 +671,40 @@ __global__ __launch_bounds__(64) void tree_wave_f32(const TreeParams p) {
     for (int r = 0; r < 4; ++r) op[16 * j + 4 * la + r] = o[j][r] * inv;
 }
 
+template <int HD, bool E8>
+hipError_t split_typed(const TreeParams& p, dim3 grid, int waves, int tpw, hipStream_t s) {
+#define SP_TREE_CASE(W_, TPW_)                                                            \
+  if (waves == W_ && tpw == TPW_) {                                                       \
+    hipLaunchKernelGGL((tree_split<HD, E8, W_, TPW_>), grid, dim3(64 * W_), 0, s, p);     \
+    return hipGetLastError();                                                             \
+  }
+  SP_TREE_CASE(1, 1) SP_TREE_CASE(2, 1) SP_TREE_CASE(3, 1) SP_TREE_CASE(4, 1)
+  SP_TREE_CASE(4, 2) SP_TREE_CASE(4, 3) SP_TREE_CASE(4, 4)
+#undef SP_TREE_CASE
+  return hipErrorInvalidValue;
+}
+
 }  // namespace
 
-hipError_t launch_tree(const TreeParams& p, int storage, int hd, int n_cus, hipStream_t s) {
-  (void)n_cus;
-  const dim3 grid((p.nodes * p.group + 15) / 16, p.st.n_kv, p.st.batch), block(64);
+hipError_t launch_tree(const TreeParams& p, int storage, int hd, hipStream_t s) {
+  const int rows = p.nodes * p.group;
   if (storage == SP_F32) {
+    const dim3 grid((rows + 15) / 16, p.st.n_kv, p.st.batch), block(64);
     if (hd == 128) hipLaunchKernelGGL((tree_wave_f32<128>), grid, block, 0, s, p);
     else hipLaunchKernelGGL((tree_wave_f32<64>), grid, block, 0, s, p);
-  } else if (storage == SP_BF16) {
-    if (hd == 128) hipLaunchKernelGGL((tree_wave<128, false>), grid, block, 0, s, p);
-    else hipLaunchKernelGGL((tree_wave<64, false>), grid, block, 0, s, p);
-  } else {
-    if (hd == 128) hipLaunchKernelGGL((tree_wave<128, true>), grid, block, 0, s, p);
-    else hipLaunchKernelGGL((tree_wave<64, true>), grid, block, 0, s, p);
+    return hipGetLastError();
   }
+  const int tpw = (p.n_tiles + p.waves - 1) / p.waves;
+  if (p.split_len % 64 || p.n_qgroups * p.n_tiles * 16 > p.r_alloc || (tpw == 1 && p.n_tiles != p.waves))
+    return hipErrorInvalidValue;
+  const dim3 grid(p.st.n_kv * p.n_qgroups, p.max_splits, p.st.batch);
+  const bool e8 = storage == SP_E4M3;
+  hipError_t e = hd == 128 ? (e8 ? split_typed<128, true>(p, grid, p.waves, tpw, s) : split_typed<128, false>(p, grid, p.waves, tpw, s))
+                           : (e8 ? split_typed<64, true>(p, grid, p.waves, tpw, s) : split_typed<64, false>(p, grid, p.waves, tpw, s));
+  if (e != hipSuccess || p.max_splits == 1) return e;
+  const dim3 mgrid((rows + 3) / 4, p.st.n_kv, p.st.batch), block(256);
+  if (hd == 128) hipLaunchKernelGGL((tree_merge<128, bf16>), mgrid, block, 0, s, p);
+  else hipLaunchKernelGGL((tree_merge<64, bf16>), mgrid, block, 0, s, p);
   return hipGetLastError();
 }
 
