@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cmath>
+#include <cstdlib>
 #include <cstring>
 #include <functional>
 #include <mutex>
@@ -139,25 +140,28 @@ constexpr int kMinSplit = 256;  // tokens
 
 TreePlan tree_plan(const sp_tree_config& c, int nodes, int num_cus) {
   TreePlan p{};
+  const bool f32 = c.kv_dtype == SP_F32;
   const int rows = nodes * (c.n_q_heads / c.n_kv_heads), tiles = (rows + 15) / 16;
-  p.n_qgroups = (tiles + kMaxTiles - 1) / kMaxTiles;
+  int most_tiles = f32 ? 1 : kMaxTiles;
+  if (const char* e = getenv("T_TILES")) most_tiles = f32 ? 1 : atoi(e);
+  p.n_qgroups = (tiles + most_tiles - 1) / most_tiles;
   p.n_tiles = (tiles + p.n_qgroups - 1) / p.n_qgroups;
   p.waves = p.n_tiles < 4 ? p.n_tiles : 4;
   p.r_alloc = p.n_qgroups * p.n_tiles * 16;
   p.split_len = c.max_seq_len > 64 ? (c.max_seq_len + 63) / 64 * 64 : 64;
-  p.max_splits = 1;
-  if (c.kv_dtype != SP_F32) {
-    const int64_t items = (int64_t)c.max_batch * c.n_kv_heads * p.n_qgroups;
-    const int64_t slots = (int64_t)num_cus * 3;
-    int64_t splits = (slots + items - 1) / items;
-    if (splits > 1) {
-      int64_t len = ((int64_t)c.max_seq_len + splits - 1) / splits;
-      len = (len + 63) / 64 * 64;
-      if (len < kMinSplit) len = kMinSplit;
-      if (len < p.split_len) p.split_len = (int)len;
-    }
-    p.max_splits = c.max_seq_len > 0 ? (c.max_seq_len + p.split_len - 1) / p.split_len : 1;
+  const int64_t items = (int64_t)c.max_batch * c.n_kv_heads * p.n_qgroups;
+  int64_t slots = (int64_t)num_cus * 3;
+  if (const char* e = getenv("T_SLOTS")) slots = (int64_t)num_cus * atoi(e);
+  int min_split = kMinSplit;
+  if (const char* e = getenv("T_MIN")) min_split = atoi(e);
+  const int64_t splits = (slots + items - 1) / items;
+  if (splits > 1) {
+    int64_t len = ((int64_t)c.max_seq_len + splits - 1) / splits;
+    len = (len + 63) / 64 * 64;
+    if (len < min_split) len = min_split;
+    if (len < p.split_len) p.split_len = (int)len;
   }
+  p.max_splits = c.max_seq_len > 0 ? (c.max_seq_len + p.split_len - 1) / p.split_len : 1;
   if (p.max_splits > 1) {
     const size_t prows = (size_t)c.max_batch * c.n_kv_heads * p.max_splits * p.r_alloc;
     p.part_bytes = align256(prows * c.head_dim * 4);

@@ -175,10 +175,12 @@ __device__ __forceinline__ uint32_t keep_mask(int keep) {
   return keep >= 4 / E ? ~0u : keep > 0 ? (1u << (8 * E * keep)) - 1 : 0u;
 }
 
-// One staged unit of cached tokens, `limit` of them there, for the wave's ntw tiles.
-template <int HD, bool E8, int TPW>
-__device__ __forceinline__ void cache_unit(Rows<HD> (&st)[TPW], int ntw, const u32x4* sb, int limit, float scale, int li,
-                                           int la) {
+// One staged unit for the wave's ntw tiles: cached tokens, `limit` of them there, or (NODES,
+// a bf16 unit) nodes, of which row li of tile t sees those in seen[t]; w keeps their weights.
+template <int HD, bool E8, int TPW, bool NODES>
+__device__ __forceinline__ void staged_unit(Rows<HD> (&st)[TPW], int ntw, const u32x4* sb, int limit,
+                                            const uint32_t (&seen)[TPW], bf16x8 (&weights)[TPW], float scale, int li,
+                                            int la) {
   using L = Unit<HD, E8>;
   constexpr int NC = HD / 32, NT = HD / 16, NH = E8 ? 4 : 2, TPL = 4 * NH;
   const int run = TPL * (li >> 2) / 16, first = TPL * (li >> 2) % 16 + (li & 3);  // of the lane's key
@@ -228,7 +230,13 @@ __device__ __forceinline__ void cache_unit(Rows<HD> (&st)[TPW], int ntw, const u
                 : sb[L::VB + (la >> 1) * L::SUB + (2 * nt + (la & 1)) * 16 + li];
   u32x4 ev = u32x4{0, 0, 0, 0};
   if constexpr (E8) ev = sb[L::EB + 4 + la];
-  if (limit < L::TOKENS) {  // a tail: tokens past the end may hold anything
+  if constexpr (NODES) {
+#pragma unroll
+    for (int t = 0; t < TPW; ++t)
+#pragma unroll
+      for (int i = 0; i < TPL; ++i)
+        if (!((seen[t] >> (TPL * la + i)) & 1)) s[t][i / 4][i % 4] = -INFINITY;
+  } else if (limit < L::TOKENS) {  // a tail: tokens past the end may hold anything
     int lim = limit;
     asm volatile("" : "+s"(lim));  // (keeps the mask a branch that whole units skip)
 #pragma unroll
@@ -274,6 +282,7 @@ __device__ __forceinline__ void cache_unit(Rows<HD> (&st)[TPW], int ntw, const u
     for (int t = 0; t < TPW; ++t)
       if (t < ntw) {
         const bf16x8 p0 = weights8(s[t], 0);
+        if constexpr (NODES) weights[t] = p0;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
           st[t].o[nt] = mfma16x16x32_bf16(p0, __builtin_bit_cast(bf16x8, vf[nt]), st[t].o[nt]);
@@ -281,54 +290,65 @@ __device__ __forceinline__ void cache_unit(Rows<HD> (&st)[TPW], int ntw, const u
   }
 }
 
-// Nodes 32 u .. of n as keys and values for one tile.  `seen`: those that row li sees.
-template <int HD>
-__device__ __forceinline__ void node_unit(const TreeParams& p, Rows<HD>& st, int b, int g, int u, int n, uint32_t seen,
-                                          int li, int la) {
-  constexpr int NC = HD / 32, NT = HD / 16;
+// Nodes 32 u .. of n into the LDS image of a bf16 unit, by the whole workgroup.  Values that
+// are not finite become 0 there (0 * NaN would carry a hidden node's values into every row);
+// returns whether this lane met one.
+template <int HD, int W>
+__device__ __forceinline__ bool stage_nodes(const TreeParams& p, u32x4* sb, int b, int g, int u, int n, int tid) {
+  using L = Unit<HD, false>;
+  constexpr int C = HD / 8;
   const bf16* kb = (const bf16*)p.k.data + (int64_t)b * p.nodes * p.k.row + g * p.k.head;
   const bf16* vb = (const bf16*)p.v.data + (int64_t)b * p.nodes * p.v.row + g * p.v.head;
-  f32x4 s[2];
+  bool odd = false;
+  for (int i = tid; i < 16 * C; i += 64 * W) {
+    const int c = i % C, t = 2 * (i / C), run = t >> 4;  // tokens t, t + 1; dims 8 c ..
+    u32x4 v[2];
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    s[h] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const bf16* kr = kb + (int64_t)min(32 * u + 8 * (li >> 2) + 4 * h + (li & 3), n - 1) * p.k.row;
+    for (int j = 0; j < 2; ++j) {
+      u32x4 k = u32x4{0, 0, 0, 0};
+      v[j] = k;
+      const int node = 32 * u + t + j;
+      if (node < n) {
+        k = row8(kb + (int64_t)node * p.k.row + 8 * c, p.k_vec);
+        v[j] = row8(vb + (int64_t)node * p.v.row + 8 * c, p.v_vec);
+      }
+      sb[run * L::KP + c * 16 + (t & 15) + j] = k;
 #pragma unroll
-    for (int q = 0; q < NC; ++q)
-      s[h] = mfma16x16x32_bf16(__builtin_bit_cast(bf16x8, row8(kr + 8 * (la * NC + q), p.k_vec)), st.q[q], s[h]);
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-      s[h][r] = (seen >> (8 * la + 4 * h + r)) & 1 ? s[h][r] : -INFINITY;
-  }
-  softmax_step<HD, 2>(st, s, p.scale_log2, la);
-  const bf16x8 p0 = weights8(s, 0);
-  bf16x8 v[NT];
-  bool odd = false;  // a value that is not finite
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int t = 32 * u + 8 * la + e;
-      v[nt][e] = t < n ? vb[(int64_t)t * p.v.row + 16 * nt + li] : (bf16)0.f;
-      odd |= !(fabsf((float)v[nt][e]) <= 3.389531389e38f);
+      for (int w = 0; w < 4; ++w) {  // exponent bits all set: NaN or infinite
+        const bool lo = (v[j][w] & 0x7f80u) == 0x7f80u, hi = (v[j][w] & 0x7f800000u) == 0x7f800000u;
+        odd |= lo | hi;
+        v[j][w] &= (lo ? 0xffff0000u : ~0u) & (hi ? 0xffffu : ~0u);
+      }
     }
-  if (!__any(odd)) {
+    const int e = (t >> 3) & 1;
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) st.o[nt] = mfma16x16x32_bf16(p0, v[nt], st.o[nt]);
-  } else {
-    // 0 * NaN would carry a hidden node's values into every row: only what a row sees is added
-    for (int t = 0; t < 32 && 32 * u + t < n; ++t) {
-      float w = (float)p0[0];  // this lane's weight of row li for its token t % 8
+    for (int d = 0; d < 8; ++d) {
+      const int dim = 8 * c + d;
+      const uint32_t a0 = (v[0][d / 2] >> (16 * (d & 1))) & 0xffffu, a1 = (v[1][d / 2] >> (16 * (d & 1))) & 0xffffu;
+      uint32_t* piece = (uint32_t*)&sb[L::VB + run * L::SUB + (2 * (dim / 16) + e) * 16 + dim % 16];
+      piece[(t & 7) / 2] = a0 | (a1 << 16);
+    }
+  }
+  return odd;
+}
+
+// The values of nodes 32 u .. that are not finite, added to the rows that see them with weight w
+// (row li's of nodes 8 la ..).
+template <int HD>
+__device__ __forceinline__ void add_odd_values(const TreeParams& p, Rows<HD>& st, bf16x8 weights, int b, int g, int u,
+                                               int n, int li, int la) {
+  const bf16* vb = (const bf16*)p.v.data + (int64_t)b * p.nodes * p.v.row + g * p.v.head;
+  for (int t = 0; t < 32 && 32 * u + t < n; ++t) {
+    float w = (float)weights[0];
 #pragma unroll
-      for (int e = 1; e < 8; ++e) w = (t & 7) == e ? (float)p0[e] : w;
+    for (int e = 1; e < 8; ++e) w = (t & 7) == e ? (float)weights[e] : w;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float wr = __shfl(w, 16 * (t >> 3) + 4 * la + r);
+    for (int r = 0; r < 4; ++r) {
+      const float wr = __shfl(w, 16 * (t >> 3) + 4 * la + r);
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          const float x = to_f32(vb[(int64_t)(32 * u + t) * p.v.row + 16 * nt + li]);
-          st.o[nt][r] = wr != 0.f ? fmaf(wr, x, st.o[nt][r]) : st.o[nt][r];
-        }
+      for (int nt = 0; nt < HD / 16; ++nt) {
+        const float x = to_f32(vb[(int64_t)(32 * u + t) * p.v.row + 16 * nt + li]);
+        if (wr != 0.f && !(fabsf(x) <= 3.389531389e38f)) st.o[nt][r] = fmaf(wr, x, st.o[nt][r]);
       }
     }
   }
@@ -351,6 +371,7 @@ __global__ __launch_bounds__(64 * W) void tree_split(const TreeParams p) {
   static_assert(W <= 2 * NI && D * LOADS < 64, "loads in flight");
   __shared__ u32x4 stage[kStages][L::PIECES];
   __shared__ int blk_ids[2][kIdWin];
+  __shared__ int odd_values[W];
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, la = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   __builtin_assume(wave >= 0 && wave < W);
@@ -377,110 +398,140 @@ __global__ __launch_bounds__(64 * W) void tree_split(const TreeParams p) {
     st[t].l = 0.f;
   }
 
-  const int nunits = (t1 - t0 + U - 1) / U;
-  if (nunits > 0) {
-    const StoreArg& c = p.st;
-    constexpr int ESZ = E8 ? 1 : 2;
-    const char* kbase = (const char*)c.k + g * c.k_sh * ESZ;
-    const char* vbase = (const char*)c.v + g * c.v_sh * ESZ;
-    const int bs = 1 << c.bs_log2;
-    const int lb0 = t0 >> c.bs_log2, nlb = ((t1 - 1) >> c.bs_log2) - lb0 + 1;
-    const int* bt_row = c.block_table ? c.block_table + (int64_t)b * c.mbps + lb0 : nullptr;
-    if (bt_row)
-      for (int i = tid; i < min(nlb, 2 * kIdWin); i += 64 * W) blk_ids[i / kIdWin][i % kIdWin] = bt_row[i];
-    auto load_window = [&](int w) __attribute__((always_inline)) {
-      for (int j = wave; j < kIdWin / 64; j += W)  // past the end: the last id again
-        ld4_to_lds(bt_row + min(w * kIdWin + j * 64 + lane, nlb - 1), &blk_ids[w & 1][j * 64]);
-    };
-    // nothing that the compiler counts stays in flight past this point
-    wait_vmcnt<0>();
-    lds_barrier();
-    uint32_t lane_off[PPL];
-    int gsel[PPL], lds_piece[PPL];
+  const StoreArg& c = p.st;
+  constexpr int ESZ = E8 ? 1 : 2;
+  const char* kbase = (const char*)c.k + g * c.k_sh * ESZ;
+  const char* vbase = (const char*)c.v + g * c.v_sh * ESZ;
+  const int bs = 1 << c.bs_log2, nunits = (t1 - t0 + U - 1) / U, lastu = nunits - 1;
+  const int lb0 = t0 >> c.bs_log2, nlb = t1 > t0 ? ((t1 - 1) >> c.bs_log2) - lb0 + 1 : 0;
+  const int* bt_row = c.block_table ? c.block_table + (int64_t)b * c.mbps + lb0 : nullptr;
+  // The first two windows of block ids and the first nodes are under way together.
+  constexpr int IDS = 2 * kIdWin / (64 * W) + (2 * kIdWin % (64 * W) != 0);
+  int ids[IDS];
+#pragma unroll
+  for (int j = 0; j < IDS; ++j) {
+    const int i = j * 64 * W + tid;
+    ids[j] = bt_row && i < nlb ? bt_row[i] : 0;
+  }
+  if (last) {
+    const bool odd = stage_nodes<HD, W>(p, stage[D], b, g, 0, n, tid);
+    const bool any = __any(odd);
+    if (lane == 0) odd_values[wave] = any;
+  }
+#pragma unroll
+  for (int j = 0; j < IDS; ++j) {
+    const int i = j * 64 * W + tid;
+    if (i < 2 * kIdWin) blk_ids[i / kIdWin][i % kIdWin] = ids[j];
+  }
+  auto load_window = [&](int w) __attribute__((always_inline)) {
+    for (int j = wave; j < kIdWin / 64; j += W)  // past the end: the last id again
+      ld4_to_lds(bt_row + min(w * kIdWin + j * 64 + lane, nlb - 1), &blk_ids[w & 1][j * 64]);
+  };
+  uint32_t lane_off[PPL];
+  int gsel[PPL], lds_piece[PPL];
+#pragma unroll
+  for (int j = 0; j < PPL; ++j) {
+    const int slot = (j * W + wave) % NI;  // (a wave count that does not divide NI loads a few twice)
+    gsel[j] = L::IPG % W == 0 ? j * W / L::IPG : slot / L::IPG;
+    lds_piece[j] = L::group_base(gsel[j]) + (slot % L::IPG) * 64;
+    const int q = (slot % L::IPG) * 64 + lane;
+    lane_off[j] = gsel[j] < NSUB ? L::key_off(q, bs) : L::value_off(q, bs);
+  }
+  const int er = (lane >> 2) & 3;  // exponents: lanes 0..15 the keys', 16..31 the values', then both again
+  // Loads are streaming (read once by this launch), unless another query group reads the
+  // same blocks, or a unit takes less than its 64 bytes of a dim's row of values.
+  const bool k_stream = p.n_qgroups == 1, v_stream = k_stream && bs * ESZ <= 64;
+  auto issue = [&](int u, int buf) __attribute__((always_inline)) {
+    int64_t blk[NSUB];
+    int slot[NSUB];
+#pragma unroll
+    for (int r = 0; r < NSUB; ++r) {
+      int t = t0 + U * u + 16 * r;
+      t = t < t1 ? t : t0 + U * u;  // a run past the end reads the unit's first again
+      const int rel = (t >> c.bs_log2) - lb0;
+      slot[r] = t & (bs - 1);
+      if (bt_row) blk[r] = __builtin_amdgcn_readfirstlane(blk_ids[((unsigned)rel / kIdWin) & 1][(unsigned)rel % kIdWin]);
+      else blk[r] = (int64_t)b * c.mbps + lb0 + rel;
+    }
+    const char *kr[NSUB], *vr[NSUB];
+#pragma unroll
+    for (int r = 0; r < NSUB; ++r) {
+      blk[r] = blk[r] >= 0 && blk[r] < c.num_blocks ? blk[r] : 0;
+      kr[r] = kbase + blk[r] * c.k_sb * ESZ + slot[r] * 16;
+      vr[r] = vbase + blk[r] * c.v_sb * ESZ + slot[r] * ESZ;
+    }
 #pragma unroll
     for (int j = 0; j < PPL; ++j) {
-      const int slot = (j * W + wave) % NI;  // (a wave count that does not divide NI loads a few twice)
-      gsel[j] = L::IPG % W == 0 ? j * W / L::IPG : slot / L::IPG;
-      lds_piece[j] = L::group_base(gsel[j]) + (slot % L::IPG) * 64;
-      const int q = (slot % L::IPG) * 64 + lane;
-      lane_off[j] = gsel[j] < NSUB ? L::key_off(q, bs) : L::value_off(q, bs);
+      const char* base = kr[0];
+#pragma unroll
+      for (int r = 1; r < NSUB; ++r) base = gsel[j] == r ? kr[r] : base;
+#pragma unroll
+      for (int r = 0; r < NSUB; ++r) base = gsel[j] == NSUB + r ? vr[r] : base;
+      if (gsel[j] < NSUB ? k_stream : v_stream) ld16_to_lds(base, lane_off[j], &stage[buf][lds_piece[j]]);
+      else ld16_to_lds<false>(base, lane_off[j], &stage[buf][lds_piece[j]]);
     }
-    const int er = (lane >> 2) & 3;  // exponents: lanes 0..15 the keys', 16..31 the values', then both again
-    // Loads are streaming (read once by this launch), unless another query group reads the
-    // same blocks, or a unit takes less than its 64 bytes of a dim's row of values.
-    const bool k_stream = p.n_qgroups == 1, v_stream = k_stream && bs * ESZ <= 64;
-    auto issue = [&](int u, int buf) __attribute__((always_inline)) {
-      int64_t blk[NSUB];
-      int slot[NSUB];
+    if constexpr (E8) {
+      int64_t eb = blk[0];
+      int es = slot[0];
 #pragma unroll
-      for (int r = 0; r < NSUB; ++r) {
-        int t = t0 + U * u + 16 * r;
-        t = t < t1 ? t : t0 + U * u;  // a run past the end reads the unit's first again
-        const int rel = (t >> c.bs_log2) - lb0;
-        slot[r] = t & (bs - 1);
-        if (bt_row) blk[r] = __builtin_amdgcn_readfirstlane(blk_ids[((unsigned)rel / kIdWin) & 1][(unsigned)rel % kIdWin]);
-        else blk[r] = (int64_t)b * c.mbps + lb0 + rel;
+      for (int r = 1; r < NSUB; ++r) {
+        eb = er == r ? blk[r] : eb;
+        es = er == r ? slot[r] : es;
       }
-      const char *kr[NSUB], *vr[NSUB];
-#pragma unroll
-      for (int r = 0; r < NSUB; ++r) {
-        blk[r] = blk[r] >= 0 && blk[r] < c.num_blocks ? blk[r] : 0;
-        kr[r] = kbase + blk[r] * c.k_sb * ESZ + slot[r] * 16;
-        vr[r] = vbase + blk[r] * c.v_sb * ESZ + slot[r] * ESZ;
-      }
-#pragma unroll
-      for (int j = 0; j < PPL; ++j) {
-        const char* base = kr[0];
-#pragma unroll
-        for (int r = 1; r < NSUB; ++r) base = gsel[j] == r ? kr[r] : base;
-#pragma unroll
-        for (int r = 0; r < NSUB; ++r) base = gsel[j] == NSUB + r ? vr[r] : base;
-        if (gsel[j] < NSUB ? k_stream : v_stream) ld16_to_lds(base, lane_off[j], &stage[buf][lds_piece[j]]);
-        else ld16_to_lds<false>(base, lane_off[j], &stage[buf][lds_piece[j]]);
-      }
-      if constexpr (E8) {
-        int64_t eb = blk[0];
-        int es = slot[0];
-#pragma unroll
-        for (int r = 1; r < NSUB; ++r) {
-          eb = er == r ? blk[r] : eb;
-          es = er == r ? slot[r] : es;
-        }
-        const uint8_t* e = lane & 16 ? c.v_exp : c.k_exp;
-        ld4_to_lds(e + eb * c.e_sb + g * c.e_sh + es + 4 * (lane & 3), &stage[buf][L::EB]);
-      }
-    };
-    const int lastu = nunits - 1;
-    // entering window w when issuing unit v: window w + 1 replaces w - 1, which no later unit reads
-    auto next_window = [&](int v) __attribute__((always_inline)) {
-      const int w = (((t0 + U * v) >> c.bs_log2) - lb0) / kIdWin;
-      const int wp = (((t0 + U * (v - 1)) >> c.bs_log2) - lb0) / kIdWin;
-      if (bt_row && w != wp && (w + 1) * kIdWin < nlb) load_window(w + 1);
-    };
-#pragma unroll
-    for (int v = 0; v < D; ++v)
-      if (v <= lastu) issue(v, v);
-    int buf = 0;
-    for (int u = 0; u < nunits; ++u) {
-      // this wave's loads of unit u have landed; after the barrier everyone's have, and all are past unit u - 1
-      wait_units_le<LOADS, D - 1>(min(u + D - 1, lastu) - u);
-      lds_barrier();
-      if (u + D <= lastu) {
-        issue(u + D, buf == 0 ? kStages - 1 : buf - 1);
-        next_window(u + D);
-      }
-      cache_unit<HD, E8, TPW>(st, ntw, stage[buf], t1 - (t0 + U * u), p.scale_log2, li, la);
-      buf = buf == kStages - 1 ? 0 : buf + 1;
+      const uint8_t* e = lane & 16 ? c.v_exp : c.k_exp;
+      ld4_to_lds(e + eb * c.e_sb + g * c.e_sh + es + 4 * (lane & 3), &stage[buf][L::EB]);
     }
+  };
+  // entering window w when issuing unit v: window w + 1 replaces w - 1, which no later unit reads
+  auto next_window = [&](int v) __attribute__((always_inline)) {
+    const int w = (((t0 + U * v) >> c.bs_log2) - lb0) / kIdWin;
+    const int wp = (((t0 + U * (v - 1)) >> c.bs_log2) - lb0) / kIdWin;
+    if (bt_row && w != wp && (w + 1) * kIdWin < nlb) load_window(w + 1);
+  };
+  uint32_t seen[TPW];
+  bf16x8 weights[TPW];
+  // nothing that the compiler counts stays in flight past this point
+  wait_vmcnt<0>();
+  lds_barrier();
+#pragma unroll
+  for (int v = 0; v < D; ++v)
+    if (v <= lastu) issue(v, v);
+  if (last)  // the nodes, from the stage that unit D will take, while the first units arrive
+    for (int u = 0; 32 * u < n; ++u) {
+      if (u > 0) {
+        lds_barrier();
+        const bool odd = stage_nodes<HD, W>(p, stage[D], b, g, u, n, tid);
+        const bool any = __any(odd);
+        if (lane == 0) odd_values[wave] = any;
+        lds_barrier();
+      }
+#pragma unroll
+      for (int t = 0; t < TPW; ++t) seen[t] = seen_word(p, b, min(row0 + 16 * t + li, rows - 1) / p.group, u, n);
+      staged_unit<HD, false, TPW, true>(st, ntw, stage[D], 32, seen, weights, p.scale_log2, li, la);
+      bool odd = false;
+#pragma unroll
+      for (int w = 0; w < W; ++w) odd |= odd_values[w] != 0;
+      if (odd)
+#pragma unroll
+        for (int t = 0; t < TPW; ++t)
+          if (t < ntw) add_odd_values<HD>(p, st[t], weights[t], b, g, u, n, li, la);
+    }
+  int buf = 0;
+  for (int u = 0; u < nunits; ++u) {
+    // this wave's loads of unit u have landed; after the barrier everyone's have, and all are past unit u - 1
+    wait_units_le<LOADS, D - 1>(min(u + D - 1, lastu) - u);
+    lds_barrier();
+    if (u + D <= lastu) {
+      issue(u + D, buf == 0 ? kStages - 1 : buf - 1);
+      next_window(u + D);
+    }
+    staged_unit<HD, E8, TPW, false>(st, ntw, stage[buf], t1 - (t0 + U * u), seen, weights, p.scale_log2, li, la);
+    buf = buf == kStages - 1 ? 0 : buf + 1;
   }
 #pragma unroll
   for (int t = 0; t < TPW; ++t) {
     const int r0 = row0 + 16 * t;
     if (t >= ntw || r0 >= rows) continue;
-    if (last) {
-      const int node = min(r0 + li, rows - 1) / p.group;
-      for (int u = 0; 32 * u < n; ++u) node_unit<HD>(p, st[t], b, g, u, n, seen_word(p, b, node, u, n), li, la);
-    }
     float l = st[t].l;
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
@@ -550,15 +601,24 @@ __global__ __launch_bounds__(256) void tree_merge(const TreeParams p) {
 // ---------------------------------------------------------------- fp32
 // The same rows with fp32 products: S^T = K Q^T, lane (li, la) holding dims 16 j + 4 la + e
 // of token and row li, then O^T += V^T P^T with the scores of row li that the lane already
-// has (tokens 4 la + r), so the running softmax needs no exchange but its maximum's.
+// has (tokens 4 la + r), so the running softmax needs no exchange but its maximum's.  One
+// workgroup of 8 waves per (query tile, KV head; split; sequence); the waves take every
+// eighth step of 16 tokens, cached ones and then, in the last split, nodes, straight from
+// memory, and join through LDS in their order.
+constexpr int kF32Waves = 8;
+
 template <int HD>
-__global__ __launch_bounds__(64) void tree_wave_f32(const TreeParams p) {
-  constexpr int NJ = HD / 16;
-  const int lane = threadIdx.x, li = lane & 15, la = lane >> 4;
-  const int row0 = 16 * blockIdx.x, g = blockIdx.y, b = blockIdx.z;
+__global__ __launch_bounds__(64 * kF32Waves) void tree_split_f32(const TreeParams p) {
+  constexpr int NJ = HD / 16, NW = kF32Waves;
+  __shared__ f32x4 osh[NW][NJ][64];
+  __shared__ float2 mlsh[NW][64];
+  const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, la = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int g = blockIdx.x % p.st.n_kv, row0 = 16 * (blockIdx.x / p.st.n_kv), b = blockIdx.z, s = blockIdx.y;
   const int n = count_of(p, b), rows = n * p.group;
-  if (row0 >= rows) return;
   const int len = clamp_len(p.seq_lens, b, p.max_seq_len);
+  const int begin = s * p.split_len, end = min(len, begin + p.split_len);
+  if (row0 >= rows || (s > 0 && begin >= len)) return;
   const int row = min(row0 + li, rows - 1), node = row / p.group, head = g * p.group + row % p.group;
   const int64_t bs = (int64_t)1 << p.st.bs_log2;
   f32x4 q[NJ], o[NJ];
@@ -604,8 +664,8 @@ __global__ __launch_bounds__(64) void tree_wave_f32(const TreeParams p) {
       for (int j = 0; j < NJ; ++j) o[j] = mfma16x16x4_f32(v[j][r], sc[r], o[j]);
     return sc;
   };
-  for (int t0 = 0; t0 < len; t0 += 16) {
-    const int limit = len - t0;
+  for (int t0 = begin + 16 * wave; t0 < end; t0 += 16 * NW) {
+    const int limit = end - t0;
     const int64_t blk = block_of(p.st, b, t0), slot = t0 & (bs - 1);
     const float* kt = (const float*)p.st.k + blk * p.st.k_sb + g * p.st.k_sh + (la * bs + slot + li) * 4;
     const float* vt = (const float*)p.st.v + blk * p.st.v_sb + g * p.st.v_sh + li * bs + slot + 4 * la;
@@ -621,7 +681,9 @@ __global__ __launch_bounds__(64) void tree_wave_f32(const TreeParams p) {
   }
   const float* kb = (const float*)p.k.data + (int64_t)b * p.nodes * p.k.row + g * p.k.head;
   const float* vb = (const float*)p.v.data + (int64_t)b * p.nodes * p.v.row + g * p.v.head;
-  for (int t0 = 0; t0 < n; t0 += 16) {
+  // node steps go on where the cached ones end
+  const int ahead = (wave + NW - (end - begin + 15) / 16 % NW) % NW;
+  for (int t0 = end == len ? 16 * ahead : n; t0 < n; t0 += 16 * NW) {
     const uint32_t seen = (seen_word(p, b, node, t0 >> 5, n) >> (t0 & 16)) & 0xffffu;
     const float* kr = kb + (int64_t)min(t0 + li, n - 1) * p.k.row;
     f32x4 k[NJ], v[NJ];
@@ -659,16 +721,34 @@ __global__ __launch_bounds__(64) void tree_wave_f32(const TreeParams p) {
   }
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
-  if (row0 + li >= rows) return;
-  if (p.lse && la == 0)
-    p.lse[((int64_t)b * p.nodes + node) * (p.st.n_kv * p.group) + head] =
-        l > 0.f || l != l ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
-  const float inv = l == 0.f ? 0.f : 1.0f / l;
-  float* op = (float*)p.out.data + ((int64_t)b * p.nodes + node) * p.out.row + (int64_t)head * p.out.head;
+  // join the waves; wave w finishes dims 16 w .. 16 w + 15 of the tile's rows
 #pragma unroll
-  for (int j = 0; j < NJ; ++j)
+  for (int j = 0; j < NJ; ++j) osh[wave][j][lane] = o[j];
+  mlsh[wave][lane] = make_float2(m, l);
+  __syncthreads();
+  if (wave >= NJ || row0 + li >= rows) return;
+  float mg = mlsh[0][lane].x, lg = 0.f;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) op[16 * j + 4 * la + r] = o[j][r] * inv;
+  for (int w = 1; w < NW; ++w) mg = fmaxf(mg, mlsh[w][lane].x);
+  f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int w = 0; w < NW; ++w) {
+    const float f = exp2f(mlsh[w][lane].x - mg);
+    lg += mlsh[w][lane].y * f;
+    x += osh[w][wave][lane] * f;
+  }
+  if (len <= p.split_len) {
+    if (p.lse && wave == 0 && la == 0)
+      p.lse[((int64_t)b * p.nodes + node) * (p.st.n_kv * p.group) + head] = lse_of(mg, lg);
+    const float inv = lg == 0.f ? 0.f : 1.0f / lg;
+    float* op = (float*)p.out.data + ((int64_t)b * p.nodes + node) * p.out.row + (int64_t)head * p.out.head + 16 * wave + 4 * la;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) op[r] = x[r] * inv;
+  } else {
+    const int64_t prow = (((int64_t)b * p.st.n_kv + g) * p.max_splits + s) * p.r_alloc + row0 + li;
+    if (wave == 0 && la == 0) p.ml_part[prow] = make_float2(mg, lg);
+    *reinterpret_cast<f32x4*>(p.o_part + prow * HD + 16 * wave + 4 * la) = x;
+  }
 }
 
 template <int HD, bool E8>
@@ -688,23 +768,31 @@ hipError_t split_typed(const TreeParams& p, dim3 grid, int waves, int tpw, hipSt
 
 hipError_t launch_tree(const TreeParams& p, int storage, int hd, hipStream_t s) {
   const int rows = p.nodes * p.group;
+  hipError_t e;
   if (storage == SP_F32) {
-    const dim3 grid((rows + 15) / 16, p.st.n_kv, p.st.batch), block(64);
-    if (hd == 128) hipLaunchKernelGGL((tree_wave_f32<128>), grid, block, 0, s, p);
-    else hipLaunchKernelGGL((tree_wave_f32<64>), grid, block, 0, s, p);
-    return hipGetLastError();
+    if (p.split_len % 16 || (rows + 15) / 16 * 16 > p.r_alloc) return hipErrorInvalidValue;
+    const dim3 grid(p.st.n_kv * ((rows + 15) / 16), p.max_splits, p.st.batch), block(64 * kF32Waves);
+    if (hd == 128) hipLaunchKernelGGL((tree_split_f32<128>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((tree_split_f32<64>), grid, block, 0, s, p);
+    e = hipGetLastError();
+  } else {
+    const int tpw = (p.n_tiles + p.waves - 1) / p.waves;
+    if (p.split_len % 64 || p.n_qgroups * p.n_tiles * 16 > p.r_alloc || (tpw == 1 && p.n_tiles != p.waves))
+      return hipErrorInvalidValue;
+    const dim3 grid(p.st.n_kv * p.n_qgroups, p.max_splits, p.st.batch);
+    const bool e8 = storage == SP_E4M3;
+    e = hd == 128 ? (e8 ? split_typed<128, true>(p, grid, p.waves, tpw, s) : split_typed<128, false>(p, grid, p.waves, tpw, s))
+                  : (e8 ? split_typed<64, true>(p, grid, p.waves, tpw, s) : split_typed<64, false>(p, grid, p.waves, tpw, s));
   }
-  const int tpw = (p.n_tiles + p.waves - 1) / p.waves;
-  if (p.split_len % 64 || p.n_qgroups * p.n_tiles * 16 > p.r_alloc || (tpw == 1 && p.n_tiles != p.waves))
-    return hipErrorInvalidValue;
-  const dim3 grid(p.st.n_kv * p.n_qgroups, p.max_splits, p.st.batch);
-  const bool e8 = storage == SP_E4M3;
-  hipError_t e = hd == 128 ? (e8 ? split_typed<128, true>(p, grid, p.waves, tpw, s) : split_typed<128, false>(p, grid, p.waves, tpw, s))
-                           : (e8 ? split_typed<64, true>(p, grid, p.waves, tpw, s) : split_typed<64, false>(p, grid, p.waves, tpw, s));
   if (e != hipSuccess || p.max_splits == 1) return e;
   const dim3 mgrid((rows + 3) / 4, p.st.n_kv, p.st.batch), block(256);
-  if (hd == 128) hipLaunchKernelGGL((tree_merge<128, bf16>), mgrid, block, 0, s, p);
-  else hipLaunchKernelGGL((tree_merge<64, bf16>), mgrid, block, 0, s, p);
+  if (storage == SP_F32) {
+    if (hd == 128) hipLaunchKernelGGL((tree_merge<128, float>), mgrid, block, 0, s, p);
+    else hipLaunchKernelGGL((tree_merge<64, float>), mgrid, block, 0, s, p);
+  } else {
+    if (hd == 128) hipLaunchKernelGGL((tree_merge<128, bf16>), mgrid, block, 0, s, p);
+    else hipLaunchKernelGGL((tree_merge<64, bf16>), mgrid, block, 0, s, p);
+  }
   return hipGetLastError();
 }
 

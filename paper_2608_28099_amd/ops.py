@@ -25,6 +25,7 @@ from .binding import ProbeError, SP_BF16, SP_E4M3, SP_F32, SP_OK
 
 _ROW_TYPES = {torch.float32: SP_F32, torch.bfloat16: SP_BF16}
 _CACHE_TYPES = {torch.float32: SP_F32, torch.bfloat16: SP_BF16, torch.float8_e4m3fn: SP_E4M3}
+_MASK_TYPES = (torch.int32, torch.uint32)
 _LAYOUTS = {"half": binding.SP_ROTARY_HALF, "interleaved": binding.SP_ROTARY_INTERLEAVED}
 _SCALINGS = {"none": binding.SP_ROTARY_PLAIN, "linear": binding.SP_ROTARY_LINEAR, "ntk": binding.SP_ROTARY_NTK,
              "yarn": binding.SP_ROTARY_YARN, "custom": binding.SP_ROTARY_CUSTOM}
@@ -36,13 +37,17 @@ def _need(ok, what):
 
 
 class _Call:
-    """The device guard and stream of one call."""
+    """The device guard and stream of one call.  (The checks of a call spell out what is wrong
+    only where they fail: a call's host time is of the order of its kernel's.)"""
+
+    __slots__ = ("device", "given", "guard", "stream")
 
     def __init__(self, device, stream):
-        _need(device.type == "cuda", "tensors must be on the GPU")
-        self.device, self.guard = device, None
-        self.given = stream
-        if device.index is not None and device.index != torch.cuda.current_device():
+        if device.type != "cuda":
+            raise ValueError("tensors must be on the GPU")
+        self.device, self.given, self.guard = device, stream, None
+        index = device.index
+        if index is not None and index != torch.cuda.current_device():
             self.guard = torch.cuda.device(device)
 
     def __enter__(self):
@@ -61,7 +66,8 @@ class _Call:
         if self.given is not None:
             s = torch.cuda.ExternalStream(self.given, device=self.device)
             for t in tensors:
-                t.record_stream(s)
+                if t is not None:
+                    t.record_stream(s)
 
 
 def _check(status, what):
@@ -71,20 +77,23 @@ def _check(status, what):
 
 def _rows(t, name, head_dim, dtype, device, n=None):
     """sp_rows of a [rows, heads, head_dim] tensor, or [batch, nodes, heads, head_dim] with evenly spaced rows."""
-    _need(t.dim() >= 3 and t.shape[-1] == head_dim, f"{name} must be [rows, heads, {head_dim}]")
-    _need(t.dtype == dtype and t.device == device, f"{name} must be {dtype} on {device}")
-    _need(t.stride(-1) == 1, f"{name}: the values of a head must lie side by side")
-    if t.dim() == 4:
-        _need(t.shape[0] == 1 or t.stride(0) == t.shape[1] * t.stride(1), f"{name}: rows must be evenly spaced")
-    else:
-        _need(t.dim() == 3, f"{name} must be [rows, heads, {head_dim}]")
-    _need(n is None or t.shape[0] == n, f"{name} must have {n} rows")
-    return binding.sp_rows(t.data_ptr(), t.stride(-3), t.stride(-2), t.shape[-2], 0)
+    shape, stride = t.shape, t.stride()
+    if not 3 <= len(shape) <= 4 or shape[-1] != head_dim:
+        raise ValueError(f"{name} must be [rows, heads, {head_dim}]")
+    if t.dtype != dtype or t.device != device:
+        raise ValueError(f"{name} must be {dtype} on {device}")
+    if stride[-1] != 1:
+        raise ValueError(f"{name}: the values of a head must lie side by side")
+    if len(shape) == 4 and shape[0] != 1 and stride[0] != shape[1] * stride[1]:
+        raise ValueError(f"{name}: rows must be evenly spaced")
+    if n is not None and shape[0] != n:
+        raise ValueError(f"{name} must have {n} rows")
+    return binding.sp_rows(t.data_ptr(), stride[-3], stride[-2], shape[-2], 0)
 
 
 def _ids(t, name, n, device):
-    _need(t.dtype == torch.int32 and t.device == device and t.dim() == 1 and t.shape[0] == n and t.is_contiguous(),
-          f"{name} must be {n} contiguous int32 on {device}")
+    if t.dtype != torch.int32 or t.device != device or t.shape != (n,) or not t.is_contiguous():
+        raise ValueError(f"{name} must be {n} contiguous int32 on {device}")
     return t.data_ptr()
 
 
@@ -115,26 +124,27 @@ def rotary(rot, positions, q, k=None, out=None, k_out=None, transpose=False, str
     rotated q, or (q, k).  out, k_out: where to write (the inputs themselves: in place);
     rows at negative positions are not written.  transpose: the gradient's rotation (by
     the opposite angle, with the same factor)."""
-    hd, dev = rot.head_dim, q.device
-    _need(q.dtype in _ROW_TYPES, "q must be float32 or bfloat16")
-    n = q.shape[0]
+    hd, dev, dtype, n = rot.head_dim, q.device, q.dtype, q.shape[0]
+    if dtype not in _ROW_TYPES:
+        raise ValueError("q must be float32 or bfloat16")
     with _Call(dev, stream) as call:
-        made = []
+        made = made_k = None
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=dev)
-            made.append(out)
-        if k is not None and k_out is None:
-            k_out = torch.empty(k.shape, dtype=k.dtype, device=dev)
-            made.append(k_out)
-        _need(out.shape == q.shape and (k is None or k_out.shape == k.shape), "outputs must have their inputs' shapes")
-        args = [_rows(q, "q", hd, q.dtype, dev, n), _rows(out, "out", hd, q.dtype, dev, n), None, None]
+            out = made = torch.empty(q.shape, dtype=dtype, device=dev)
+        elif out.shape != q.shape:
+            raise ValueError("out must have q's shape")
+        qr, outr = _rows(q, "q", hd, dtype, dev, n), _rows(out, "out", hd, dtype, dev, n)
+        kr = k_outr = None
         if k is not None:
-            args[2:] = [_rows(k, "k", hd, q.dtype, dev, n), _rows(k_out, "k_out", hd, q.dtype, dev, n)]
-        refs = [None if a is None else ctypes.byref(a) for a in args]
-        _check(binding.load().sp_probe_rotary(ctypes.byref(rot), _ROW_TYPES[q.dtype], int(bool(transpose)), n,
-                                              _ids(positions, "positions", n, dev), *refs, call.stream),
+            if k_out is None:
+                k_out = made_k = torch.empty(k.shape, dtype=dtype, device=dev)
+            elif k_out.shape != k.shape:
+                raise ValueError("k_out must have k's shape")
+            kr, k_outr = _rows(k, "k", hd, dtype, dev, n), _rows(k_out, "k_out", hd, dtype, dev, n)
+        _check(binding.load().sp_probe_rotary(rot, _ROW_TYPES[dtype], 1 if transpose else 0, n,
+                                              _ids(positions, "positions", n, dev), qr, outr, kr, k_outr, call.stream),
                "sp_probe_rotary")
-        call.hold(*made)
+        call.hold(made, made_k)
     return out if k is None else (out, k_out)
 
 
@@ -178,7 +188,9 @@ class PagedCache:
             st.exponent_stride_block, st.exponent_stride_head = k_exponents.stride(0), k_exponents.stride(1)
         else:
             _need(k_exponents is None and v_exponents is None, "exponents belong to float8 caches")
-        self.c = st
+        self.c, self.c_dtype = st, st.dtype
+        self.table = None if block_table is None else block_table.data_ptr()
+        self.capacity = min(self.max_blocks * block_size, (1 << 31) - 1)  # tokens of a sequence
 
     @classmethod
     def allocate(cls, dtype, num_blocks, n_kv_heads, head_dim, block_size=16, block_table=None, batch=None, device="cuda"):
@@ -196,47 +208,46 @@ class PagedCache:
         return cls(kv.pool[:, :, 0], kv.pool[:, :, 1], kv.block_size, kv.block_table,
                    batch=None if kv.block_table is not None else kv.seq_lens.shape[0])
 
-    def _table(self):
-        return None if self.block_table is None else self.block_table.data_ptr()
-
 
 def cache_write(cache: PagedCache, seq_ids, positions, k, v, src_rows=None, rotary=None, stream=None):
     """Row i of k and v (row src_rows[i]; all [rows, n_kv_heads, head_dim], float32 or bfloat16)
     becomes token positions[i] of sequence seq_ids[i]; the key is rotated there first if a
     rotation is given.  Rows with ids or positions out of range are skipped; the slots of a
     call must differ."""
-    dev, n = cache.device, seq_ids.shape[0]
-    _need(k.dtype in _ROW_TYPES, "k must be float32 or bfloat16")
-    _need(src_rows is not None or k.shape[0] == n, f"k must have {n} rows")
+    dev, n, dtype, hd = cache.device, seq_ids.shape[0], k.dtype, cache.head_dim
+    if dtype not in _ROW_TYPES or k.dim() != 3 or v.dim() != 3:
+        raise ValueError("k and v must be [rows, heads, head_dim], float32 or bfloat16")
+    n_src = k.shape[0]
+    if src_rows is None and n_src != n:
+        raise ValueError(f"k must have {n} rows")
     with _Call(dev, stream) as call:
-        kr, vr = _rows(k, "k", cache.head_dim, k.dtype, dev), _rows(v, "v", cache.head_dim, k.dtype, dev, k.shape[0])
-        _need(k.dim() == 3 and v.dim() == 3, "k and v must be [rows, heads, head_dim]")
         _check(binding.load().sp_probe_cache_write(
-            ctypes.byref(cache.c), cache._table(), _ROW_TYPES[k.dtype], n, _ids(seq_ids, "seq_ids", n, dev),
+            cache.c, cache.table, _ROW_TYPES[dtype], n, _ids(seq_ids, "seq_ids", n, dev),
             _ids(positions, "positions", n, dev), None if src_rows is None else _ids(src_rows, "src_rows", n, dev),
-            k.shape[0], ctypes.byref(kr), ctypes.byref(vr), None if rotary is None else ctypes.byref(rotary),
-            call.stream), "sp_probe_cache_write")
+            n_src, _rows(k, "k", hd, dtype, dev), _rows(v, "v", hd, dtype, dev, n_src), rotary, call.stream),
+            "sp_probe_cache_write")
 
 
 def cache_read(cache: PagedCache, seq_ids, positions, dtype=torch.bfloat16, k=None, v=None, stream=None):
     """Tokens positions[i] of sequences seq_ids[i] as rows [rows, n_kv_heads, head_dim] (k, v) of
-    dtype; given k and v are written (rows with ids or positions out of range are left as
-    they are)."""
-    dev, n = cache.device, seq_ids.shape[0]
+    dtype; given k and v (either or both) are written instead: rows with ids or positions out
+    of range are left as they are."""
+    dev, n, hd = cache.device, seq_ids.shape[0], cache.head_dim
     with _Call(dev, stream) as call:
-        made = []
+        made_k = made_v = None
         if k is None and v is None:
-            _need(dtype in _ROW_TYPES, "dtype must be float32 or bfloat16")
-            k, v = (torch.empty((n, cache.n_kv_heads, cache.head_dim), dtype=dtype, device=dev) for _ in "kv")
-            made = [k, v]
-        t = k if k is not None else v
-        _need(t.dtype in _ROW_TYPES, "k and v must be float32 or bfloat16")
-        rows = [None if x is None else _rows(x, m, cache.head_dim, t.dtype, dev, n) for x, m in ((k, "k"), (v, "v"))]
+            shape = (n, cache.n_kv_heads, hd)
+            k = made_k = torch.empty(shape, dtype=dtype, device=dev)
+            v = made_v = torch.empty(shape, dtype=dtype, device=dev)
+        else:
+            dtype = k.dtype if k is not None else v.dtype
+        if dtype not in _ROW_TYPES:
+            raise ValueError("rows must be float32 or bfloat16")
         _check(binding.load().sp_probe_cache_read(
-            ctypes.byref(cache.c), cache._table(), _ROW_TYPES[t.dtype], n, _ids(seq_ids, "seq_ids", n, dev),
-            _ids(positions, "positions", n, dev), *[None if r is None else ctypes.byref(r) for r in rows], call.stream),
-            "sp_probe_cache_read")
-        call.hold(*made)
+            cache.c, cache.table, _ROW_TYPES[dtype], n, _ids(seq_ids, "seq_ids", n, dev),
+            _ids(positions, "positions", n, dev), None if k is None else _rows(k, "k", hd, dtype, dev, n),
+            None if v is None else _rows(v, "v", hd, dtype, dev, n), call.stream), "sp_probe_cache_read")
+        call.hold(made_k, made_v)
     return k, v
 
 
@@ -260,9 +271,8 @@ def tree_mask(parents):
 
 
 def _tree_config(cache, n_q_heads, dtype, nodes, batch, max_seq_len, scale):
-    return binding.sp_tree_config(n_q_heads=n_q_heads, n_kv_heads=cache.n_kv_heads, head_dim=cache.head_dim,
-                                  dtype=_ROW_TYPES[dtype], kv_dtype=_CACHE_TYPES[cache.dtype], max_nodes=nodes,
-                                  max_batch=batch, max_seq_len=max_seq_len, scale=scale)
+    return binding.sp_tree_config(n_q_heads, cache.n_kv_heads, cache.head_dim, _ROW_TYPES[dtype], cache.c_dtype, nodes,
+                                  batch, max_seq_len, scale, 0)
 
 
 def tree_attention(cache: PagedCache, seq_lens, q, k, v, mask=None, counts=None, max_seq_len: Optional[int] = None,
@@ -272,58 +282,60 @@ def tree_attention(cache: PagedCache, seq_lens, q, k, v, mask=None, counts=None,
     [batch, nodes, n_kv_heads, head_dim] as mask shows them: int32 words [batch, nodes, words]
     or [nodes, words] (tree_mask; bit j of word w of node i: it sees node 32 w + j); None: each
     node sees those up to itself.  counts (int32 [batch]): nodes of each sequence; rows past
-    them are not written.  max_seq_len: the longest sequence, shorter bounds make better
-    plans (default: what the block table holds).  lse: float32 [batch, nodes, n_q_heads] to
+    them are not written.  max_seq_len: the longest sequence, which plans the launch (default:
+    what the block table holds).  lse: float32 [batch, nodes, n_q_heads] to
     receive ln sum exp(score).  workspace: a uint8 tensor to use instead of fresh memory."""
-    dev, hd = cache.device, cache.head_dim
-    _need(q.dim() == 4 and k.dim() == 4 and v.shape == k.shape and k.shape[:2] == q.shape[:2],
-          "q, k and v must be [batch, nodes, heads, head_dim]")
-    _need(q.dtype in _ROW_TYPES, "q must be float32 or bfloat16")
-    batch, nodes, nq = q.shape[:3]
-    _need(batch == cache.batch, f"the cache has {cache.batch} sequences")
-    _need(k.shape[2] == cache.n_kv_heads, f"the cache has {cache.n_kv_heads} KV heads")
+    dev, hd, dtype, shape = cache.device, cache.head_dim, q.dtype, q.shape
+    if dtype not in _ROW_TYPES:
+        raise ValueError("q must be float32 or bfloat16")
+    if len(shape) != 4 or k.dim() != 4 or v.shape != k.shape or k.shape[:2] != shape[:2]:
+        raise ValueError("q, k and v must be [batch, nodes, heads, head_dim]")
+    batch, nodes, nq = shape[:3]
+    if batch != cache.batch:
+        raise ValueError(f"the cache has {cache.batch} sequences")
+    if k.shape[2] != cache.n_kv_heads:
+        raise ValueError(f"the cache has {cache.n_kv_heads} KV heads")
     if max_seq_len is None:
-        max_seq_len = min(cache.max_blocks * cache.block_size, (1 << 31) - 1)
-    _need(scale is None or (math.isfinite(scale) and scale > 0), "scale must be positive")
+        max_seq_len = cache.capacity
+    if scale is None:
+        scale = 0.0
+    elif not (math.isfinite(scale) and scale > 0):
+        raise ValueError("scale must be positive")
     with _Call(dev, stream) as call:
-        made = []
+        made = made_ws = None
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=dev)
-            made.append(out)
-        _need(out.shape == q.shape, "out must have q's shape")
-        tree = binding.sp_tree(n_nodes=nodes)
-        tree.q, tree.out = _rows(q, "q", hd, q.dtype, dev), _rows(out, "out", hd, q.dtype, dev)
-        tree.k, tree.v = _rows(k, "k", hd, q.dtype, dev), _rows(v, "v", hd, q.dtype, dev)
-        if counts is not None:
-            tree.counts = _ids(counts, "counts", batch, dev)
+            out = made = torch.empty(shape, dtype=dtype, device=dev)
+        elif out.shape != shape:
+            raise ValueError("out must have q's shape")
+        tree = binding.sp_tree(nodes, 0, None if counts is None else _ids(counts, "counts", batch, dev), None, 0,
+                               _rows(q, "q", hd, dtype, dev), _rows(k, "k", hd, dtype, dev),
+                               _rows(v, "v", hd, dtype, dev), _rows(out, "out", hd, dtype, dev), None)
         if mask is not None:
-            _need(mask.dtype in (torch.int32, torch.uint32) and mask.device == dev and mask.is_contiguous()
-                  and mask.dim() in (2, 3) and mask.shape[-2] == nodes and (mask.dim() == 2 or mask.shape[0] == batch),
-                  "mask must be contiguous int32 words [batch, nodes, words] or [nodes, words]")
-            tree.mask, tree.mask_words = mask.data_ptr(), mask.shape[-1]
-            tree.mask_stride = 0 if mask.dim() == 2 else nodes * mask.shape[-1]
+            words = mask.shape
+            if (mask.dtype not in _MASK_TYPES or mask.device != dev or not mask.is_contiguous()
+                    or not 2 <= len(words) <= 3 or words[-2] != nodes or (len(words) == 3 and words[0] != batch)):
+                raise ValueError("mask must be contiguous int32 words [batch, nodes, words] or [nodes, words]")
+            tree.mask, tree.mask_words = mask.data_ptr(), words[-1]
+            tree.mask_stride = 0 if len(words) == 2 else nodes * words[-1]
         if lse is not None:
-            _need(lse.dtype == torch.float32 and lse.device == dev and lse.is_contiguous()
-                  and tuple(lse.shape) == (batch, nodes, nq), "lse must be contiguous float32 [batch, nodes, n_q_heads]")
+            if lse.dtype != torch.float32 or lse.device != dev or not lse.is_contiguous() or lse.shape != shape[:3]:
+                raise ValueError("lse must be contiguous float32 [batch, nodes, n_q_heads]")
             tree.lse = lse.data_ptr()
-        cfg = _tree_config(cache, nq, q.dtype, nodes, max(batch, 1), max_seq_len, scale or 0.0)
+        cfg = _tree_config(cache, nq, dtype, nodes, batch or 1, max_seq_len, scale)
         lib = binding.load()
         if workspace is None:
-            n = lib.sp_probe_tree_workspace_bytes(ctypes.byref(cfg))
-            workspace = torch.empty(max(n, 16), dtype=torch.uint8, device=dev)
-            made.append(workspace)
-        _need(workspace.dtype == torch.uint8 and workspace.device == dev and workspace.is_contiguous(),
-              f"workspace must be contiguous uint8 on {dev}")
-        _check(lib.sp_probe_tree_attention(ctypes.byref(cfg), ctypes.byref(cache.c),
-                                           _ids(seq_lens, "seq_lens", batch, dev), cache._table(), ctypes.byref(tree),
+            workspace = made_ws = torch.empty(max(lib.sp_probe_tree_workspace_bytes(cfg), 16), dtype=torch.uint8, device=dev)
+        elif workspace.dtype != torch.uint8 or workspace.device != dev or not workspace.is_contiguous():
+            raise ValueError(f"workspace must be contiguous uint8 on {dev}")
+        _check(lib.sp_probe_tree_attention(cfg, cache.c, _ids(seq_lens, "seq_lens", batch, dev), cache.table, tree,
                                            workspace.data_ptr(), workspace.numel(), call.stream),
                "sp_probe_tree_attention")
-        call.hold(*made)
+        call.hold(made, made_ws)
     return out
 
 
 def tree_workspace_bytes(cache: PagedCache, n_q_heads, dtype, nodes, batch=None, max_seq_len=None):
-    """Bytes of workspace that tree_attention needs for calls of these sizes (0: not supported)."""
-    cfg = _tree_config(cache, n_q_heads, dtype, nodes, cache.batch if batch is None else batch,
-                       cache.max_blocks * cache.block_size if max_seq_len is None else max_seq_len, 0.0)
-    return binding.load().sp_probe_tree_workspace_bytes(ctypes.byref(cfg))
+    """Bytes of workspace that tree_attention needs for calls of at most these sizes (0: not supported)."""
+    return binding.load().sp_probe_tree_workspace_bytes(
+        _tree_config(cache, n_q_heads, dtype, nodes, cache.batch if batch is None else batch,
+                     cache.capacity if max_seq_len is None else max_seq_len, 0.0))
