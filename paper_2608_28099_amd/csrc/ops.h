@@ -62,12 +62,13 @@ struct TreeParams {
   float* lse;                    // nullable
   int nodes, group, max_seq_len;
   float scale_log2;              // the scores' factor times log2(e)
-  // the plan: query rows in n_qgroups groups of n_tiles tiles of 16 (r_alloc rows in all), one
-  // workgroup of `waves` waves each; splits of split_len tokens, max_splits of max_seq_len
-  int n_qgroups, n_tiles, waves, r_alloc, split_len, max_splits;
-  float* o_part;                 // [B][n_kv][max_splits][r_alloc][hd], not divided by the sum
+  // the plan: query rows in n_qgroups groups of 64 (fp32: 16), a workgroup each, r_alloc rows in
+  // all; splits of split_len tokens, max_splits of max_seq_len
+  int n_qgroups, r_alloc, split_len, max_splits;
+  float* o_part;                 // [B][n_kv][max_splits][r_alloc / 16][16 hd], not divided by the sum
   float2* ml_part;               // [B][n_kv][max_splits][r_alloc]: maximum (log2 units), sum
 };
+constexpr int kTreeRows = 64, kTreeRowsF32 = 16;  // query rows of a workgroup
 hipError_t launch_tree(const TreeParams& p, int storage, int hd, hipStream_t s);
 
 }  // namespace sp

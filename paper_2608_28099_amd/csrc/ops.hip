@@ -3,7 +3,6 @@
 #include <hip/hip_runtime.h>
 
 #include <cmath>
-#include <cstdlib>
 #include <cstring>
 #include <functional>
 #include <mutex>
@@ -128,40 +127,43 @@ int check_tree_config(const sp_tree_config* c) {
 // How a call of `nodes` nodes is laid out on num_cus compute units.  The splits follow the
 // config's max_batch, so that its workspace holds every call's partial results.
 struct TreePlan {
-  int n_qgroups, n_tiles, waves, r_alloc, split_len, max_splits;
+  int n_qgroups, r_alloc, split_len, max_splits;
   size_t part_bytes;  // of O; the (m, l) pairs follow
   size_t total;
 };
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-constexpr int kMaxTiles = 16;   // query tiles per workgroup: 4 waves of 4
 constexpr int kMinSplit = 256;  // tokens
 
 TreePlan tree_plan(const sp_tree_config& c, int nodes, int num_cus) {
   TreePlan p{};
-  const bool f32 = c.kv_dtype == SP_F32;
-  const int rows = nodes * (c.n_q_heads / c.n_kv_heads), tiles = (rows + 15) / 16;
-  int most_tiles = f32 ? 1 : kMaxTiles;
-  if (const char* e = getenv("T_TILES")) most_tiles = f32 ? 1 : atoi(e);
-  p.n_qgroups = (tiles + most_tiles - 1) / most_tiles;
-  p.n_tiles = (tiles + p.n_qgroups - 1) / p.n_qgroups;
-  p.waves = p.n_tiles < 4 ? p.n_tiles : 4;
-  p.r_alloc = p.n_qgroups * p.n_tiles * 16;
-  p.split_len = c.max_seq_len > 64 ? (c.max_seq_len + 63) / 64 * 64 : 64;
+  const int rows = nodes * (c.n_q_heads / c.n_kv_heads), per = c.kv_dtype == SP_F32 ? kTreeRowsF32 : kTreeRows;
+  p.n_qgroups = (rows + per - 1) / per;
+  p.r_alloc = p.n_qgroups * per;
   const int64_t items = (int64_t)c.max_batch * c.n_kv_heads * p.n_qgroups;
-  int64_t slots = (int64_t)num_cus * 3;
-  if (const char* e = getenv("T_SLOTS")) slots = (int64_t)num_cus * atoi(e);
-  int min_split = kMinSplit;
-  if (const char* e = getenv("T_MIN")) min_split = atoi(e);
-  const int64_t splits = (slots + items - 1) / items;
-  if (splits > 1) {
-    int64_t len = ((int64_t)c.max_seq_len + splits - 1) / splits;
-    len = (len + 63) / 64 * 64;
-    if (len < min_split) len = min_split;
-    if (len < p.split_len) p.split_len = (int)len;
+  const int64_t n = c.max_seq_len, slots = (int64_t)num_cus * 3;  // three workgroups per compute unit, by LDS
+  // As many splits as fill the device once, and pieces of at most an eighth of the longest sequence
+  // (or 2048 tokens): a batch of long and short sequences takes several rounds, whose ends level
+  // out (64 sequences of 2K-32K tokens, 320 rows: 1315-1345 us in splits of 4096-8192, 1655 of 1024,
+  // 1570 unsplit).  Then up to as many again, until the last round is full: of alike
+  // sequences a round that a third of the device works on costs a whole one (32 of 131072
+  // tokens, 4 rows: 1485 us in 4 splits each, 1.33 rounds; 1350 in 8, 2.67; 1372 in 3, one).
+  const int64_t fill = (n * items + slots - 1) / slots, cap = n / 8 > 2048 ? n / 8 : 2048;
+  int64_t len = fill < cap ? fill : cap;
+  if (len < kMinSplit) len = kMinSplit;
+  const int64_t k0 = n > len ? (n + len - 1) / len : 1;
+  int64_t best = k0;
+  double least = 1e30;
+  for (int64_t k = k0; k0 > 1 && k <= 2 * k0 && least > 1.1; ++k) {
+    const double rounds = (double)(items * k) / (double)slots, waste = std::ceil(rounds) / rounds;
+    if (n / k < kMinSplit) break;
+    if (waste < least) { least = waste; best = k; }
   }
-  p.max_splits = c.max_seq_len > 0 ? (c.max_seq_len + p.split_len - 1) / p.split_len : 1;
+  len = (n + best - 1) / best;
+  if (len < 1) len = 1;
+  p.split_len = (int)((len + 63) / 64 * 64);
+  p.max_splits = n > 0 ? (int)((n + p.split_len - 1) / p.split_len) : 1;
   if (p.max_splits > 1) {
     const size_t prows = (size_t)c.max_batch * c.n_kv_heads * p.max_splits * p.r_alloc;
     p.part_bytes = align256(prows * c.head_dim * 4);
@@ -172,14 +174,14 @@ TreePlan tree_plan(const sp_tree_config& c, int nodes, int num_cus) {
 }
 
 // The largest plan of the calls that c allows: splits change with the number of query groups only,
-// and with that number the rows grow with the nodes.
+// and within one number of groups every plan is alike.
 size_t tree_workspace(const sp_tree_config& c, int num_cus) {
-  const int group = c.n_q_heads / c.n_kv_heads;
+  const int group = c.n_q_heads / c.n_kv_heads, per = c.kv_dtype == SP_F32 ? kTreeRowsF32 : kTreeRows;
   size_t most = tree_plan(c, c.max_nodes, num_cus).total;
-  for (int q = 1; 16 * kMaxTiles * q / group < c.max_nodes; ++q) {  // the most nodes of q groups
-    const int nodes = 16 * kMaxTiles * q / group;
-    const size_t n = nodes > 0 ? tree_plan(c, nodes, num_cus).total : 0;
-    most = n > most ? n : most;
+  for (int q = 1; per * q / group < c.max_nodes; ++q) {  // the most nodes of q groups
+    const int nodes = per * q / group;
+    const size_t x = nodes > 0 ? tree_plan(c, nodes, num_cus).total : 0;
+    most = x > most ? x : most;
   }
   return most;
 }
@@ -381,8 +383,6 @@ SP_API int sp_probe_tree_attention(const sp_tree_config* c, const sp_kv_store* s
   if (workspace_bytes < pl.total) return SP_ERR_INVALID_ARG;
   if (st != SP_OK) return st;
   p.n_qgroups = pl.n_qgroups;
-  p.n_tiles = pl.n_tiles;
-  p.waves = pl.waves;
   p.r_alloc = pl.r_alloc;
   p.split_len = pl.split_len;
   p.max_splits = pl.max_splits;

@@ -16,6 +16,8 @@
 // 64) for 8-bit caches, so that either reads 16 bytes per lane at a time.  8-bit keys become
 // bf16 with their exponent, exactly; the values' exponents go to the weights instead,
 // exactly too (a power of two).
+#include <type_traits>
+
 #include "common.h"
 #include "ops.h"
 
@@ -55,18 +57,18 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 // 8 E4M3 values (two words) to bf16, times a power of two.
 __device__ __forceinline__ bf16x8 from_e4m3(uint32_t a, uint32_t b, float scale) {
-  const bf16x2 w0 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, false);
-  const bf16x2 w1 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, true);
-  const bf16x2 w2 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false);
-  const bf16x2 w3 = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true);
-  return bf16x8{w0[0], w0[1], w1[0], w1[1], w2[0], w2[1], w3[0], w3[1]};
+  return __builtin_bit_cast(
+      bf16x8, u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, false)),
+                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, true)),
+                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false)),
+                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true))});
 }
 __device__ __forceinline__ float exponent_scale(uint32_t byte) {
   return __builtin_bit_cast(float, byte << 23);
 }
 
 template <int HD>
-struct Rows {  // 16 query rows of a wave
+struct Rows {  // a wave's 16 query rows
   static constexpr int NC = HD / 32, NT = HD / 16;
   bf16x8 q[NC];   // Q[row li][8 (la NC + c) ..]
   f32x4 o[NT];    // O[row 4 la + r][16 nt + li]
@@ -78,10 +80,10 @@ struct Rows {  // 16 query rows of a wave
 // across lanes and the rescaling of O.
 constexpr float kRescaleLog2 = 8.0f;
 
-// The lane's scores s (products not yet scaled; masked ones -inf) of NH * 4 tokens become
-// weights 2^(s scale - m); where the maximum moves, l and o follow.
+// Moves a row's reference maximum (and l and o with it) where one of the lane's scores s (products
+// not yet scaled, masked ones -inf) exceeds it by too much.
 template <int HD, int NH>
-__device__ __forceinline__ void softmax_step(Rows<HD>& st, f32x4 (&s)[NH], float scale, int la) {
+__device__ __forceinline__ void raise_maximum(Rows<HD>& st, const f32x4 (&s)[NH], float scale, int la) {
   float mx = fmaxf(s[0][0], s[0][1]);
 #pragma unroll
   for (int i = 2; i < 4 * NH; ++i) mx = fmaxf(mx, s[i / 4][i % 4]);
@@ -101,13 +103,6 @@ __device__ __forceinline__ void softmax_step(Rows<HD>& st, f32x4 (&s)[NH], float
 #pragma unroll
       for (int r = 0; r < 4; ++r) st.o[nt][r] *= ar[r];
   }
-#pragma unroll
-  for (int h = 0; h < NH; ++h)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      s[h][r] = fast_exp2(fmaf(s[h][r], scale, -st.m));
-      st.l += s[h][r];
-    }
 }
 
 // The weights of 8 tokens (scores h0 and h0 + 1) as a bf16 operand.  Rounded to nearest:
@@ -135,11 +130,9 @@ struct Unit {
   static constexpr int NSUB = E8 ? 4 : 2, TOKENS = 16 * NSUB;
   static constexpr int SUB = E8 ? HD : 2 * HD;       // pieces of a run's keys, or of its values
   static constexpr int KP = SUB + 4, VB = NSUB * KP;
-  static constexpr int EB = VB + NSUB * SUB;         // exponents: 64 words (keys 16, values 16, twice)
-  static constexpr int PIECES = EB + (E8 ? 16 : 0);
-  static constexpr int IPG = SUB / 64;               // loads of 64 pieces per run
-  static constexpr int NI = 2 * NSUB * IPG;          // per unit
-  static __device__ __forceinline__ int group_base(int gi) { return gi < NSUB ? gi * KP : VB + (gi - NSUB) * SUB; }
+  static constexpr int EB = VB + NSUB * SUB;         // exponents: per run 4 words the keys', 4 the values'
+  static constexpr int PIECES = EB + (E8 ? 2 * NSUB : 0);
+  static constexpr int IPG = SUB / 64;               // loads of 64 pieces per run's keys, or its values
   // byte offset of piece q of a run from its first token's place in the block
   static __device__ __forceinline__ uint32_t key_off(int q, int bs) { return (uint32_t)((q >> 4) * bs + (q & 15)) * 16u; }
   static __device__ __forceinline__ uint32_t value_off(int q, int bs) {
@@ -150,23 +143,11 @@ struct Unit {
 
 // Physical block ids of a split: two windows of kIdWin logical blocks, window w in half w & 1.
 constexpr int kIdWin = 256;
-constexpr int kStages = 3;
 
 // Direct 4-byte loads into LDS: lane l's word lands at dst + 4 l (dst uniform).
 __device__ __forceinline__ void ld4_to_lds(const void* addr, void* dst) {
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)dst;
   asm volatile("global_load_lds_dword %0, off" : : "v"(addr), "{m0}"(lds) : "memory");
-}
-
-// Wait until at most k units of PPL loads each remain in flight (k <= K).
-template <int PPL, int K>
-__device__ __forceinline__ void wait_units_le(int k) {
-  if constexpr (K == 0) {
-    wait_vmcnt<0>();
-  } else {
-    if (k >= K) wait_vmcnt<K * PPL>();
-    else wait_units_le<PPL, K - 1>(k);
-  }
 }
 
 // Bits of a word of E bytes per value whose first token is `keep` tokens before the end.
@@ -175,118 +156,95 @@ __device__ __forceinline__ uint32_t keep_mask(int keep) {
   return keep >= 4 / E ? ~0u : keep > 0 ? (1u << (8 * E * keep)) - 1 : 0u;
 }
 
-// One staged unit for the wave's ntw tiles: cached tokens, `limit` of them there, or (NODES,
-// a bf16 unit) nodes, of which row li of tile t sees those in seen[t]; w keeps their weights.
-template <int HD, bool E8, int TPW, bool NODES>
-__device__ __forceinline__ void staged_unit(Rows<HD> (&st)[TPW], int ntw, const u32x4* sb, int limit,
-                                            const uint32_t (&seen)[TPW], bf16x8 (&weights)[TPW], float scale, int li,
-                                            int la) {
+// Scores of a staged unit, not scaled.
+template <int HD, bool E8>
+__device__ __forceinline__ void unit_scores(const Rows<HD>& st, f32x4 (&s)[E8 ? 4 : 2], const u32x4* sb, int li, int la) {
   using L = Unit<HD, E8>;
-  constexpr int NC = HD / 32, NT = HD / 16, NH = E8 ? 4 : 2, TPL = 4 * NH;
+  constexpr int NC = HD / 32, NH = E8 ? 4 : 2, TPL = 4 * NH;
   const int run = TPL * (li >> 2) / 16, first = TPL * (li >> 2) % 16 + (li & 3);  // of the lane's key
-  f32x4 s[TPW][NH];
 #pragma unroll
-  for (int t = 0; t < TPW; ++t)
-#pragma unroll
-    for (int h = 0; h < NH; ++h) s[t][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int h = 0; h < NH; ++h) s[h] = f32x4{0.f, 0.f, 0.f, 0.f};
   if constexpr (E8) {
-    const u32x4 ek = sb[L::EB + run];
+    const u32x4 ek = sb[L::EB + 2 * run];
 #pragma unroll
     for (int h = 0; h < NH; ++h) {
       const float f = exponent_scale((ek[h] >> (8 * (li & 3))) & 0xffu);
 #pragma unroll
       for (int q = 0; q < NC / 2; ++q) {
         const u32x4 w = sb[run * L::KP + (la * (NC / 2) + q) * 16 + first + 4 * h];
-        const bf16x8 k0 = from_e4m3(w[0], w[1], f), k1 = from_e4m3(w[2], w[3], f);
-#pragma unroll
-        for (int t = 0; t < TPW; ++t)
-          if (t < ntw) {
-            s[t][h] = mfma16x16x32_bf16(k0, st[t].q[2 * q], s[t][h]);
-            s[t][h] = mfma16x16x32_bf16(k1, st[t].q[2 * q + 1], s[t][h]);
-          }
+        s[h] = mfma16x16x32_bf16(from_e4m3(w[0], w[1], f), st.q[2 * q], s[h]);
+        s[h] = mfma16x16x32_bf16(from_e4m3(w[2], w[3], f), st.q[2 * q + 1], s[h]);
       }
     }
   } else {
-    u32x4 kf[NH][NC];
 #pragma unroll
-    for (int h = 0; h < NH; ++h)
+    for (int q = 0; q < NC; ++q)
 #pragma unroll
-      for (int q = 0; q < NC; ++q) kf[h][q] = sb[run * L::KP + (la * NC + q) * 16 + first + 4 * h];
-#pragma unroll
-    for (int t = 0; t < TPW; ++t)
-      if (t < ntw)
-#pragma unroll
-        for (int q = 0; q < NC; ++q)
-#pragma unroll
-          for (int h = 0; h < NH; ++h)
-            s[t][h] = mfma16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[h][q]), st[t].q[q], s[t][h]);
+      for (int h = 0; h < NH; ++h)
+        s[h] = mfma16x16x32_bf16(__builtin_bit_cast(bf16x8, sb[run * L::KP + (la * NC + q) * 16 + first + 4 * h]),
+                                 st.q[q], s[h]);
   }
-  // values are read once the scores' products are issued, into registers the keys held
-  __builtin_amdgcn_sched_barrier(0);
-  u32x4 vf[NT];
+}
+
+// Tokens at or past `limit` of the lane's scores become -inf.
+template <int NH>
+__device__ __forceinline__ void mask_tail(f32x4 (&s)[NH], int limit, int la) {
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt)
-    vf[nt] = E8 ? sb[L::VB + la * L::SUB + 16 * nt + li]
-                : sb[L::VB + (la >> 1) * L::SUB + (2 * nt + (la & 1)) * 16 + li];
-  u32x4 ev = u32x4{0, 0, 0, 0};
-  if constexpr (E8) ev = sb[L::EB + 4 + la];
-  if constexpr (NODES) {
+  for (int i = 0; i < 4 * NH; ++i)
+    if (4 * NH * la + i >= limit) s[i / 4][i % 4] = -INFINITY;
+}
+
+// The lane's fragments of a staged unit's values, and their exponents.  Tokens at or past `limit`
+// may hold anything and become 0.
+template <int HD, bool E8>
+struct Values {
+  u32x4 v[HD / 16], e;
+};
+template <int HD, bool E8>
+__device__ __forceinline__ void read_values(Values<HD, E8>& x, const u32x4* sb, int li, int la) {
+  using L = Unit<HD, E8>;
 #pragma unroll
-    for (int t = 0; t < TPW; ++t)
+  for (int nt = 0; nt < HD / 16; ++nt)
+    x.v[nt] = E8 ? sb[L::VB + la * L::SUB + 16 * nt + li]
+                 : sb[L::VB + (la >> 1) * L::SUB + (2 * nt + (la & 1)) * 16 + li];
+  if constexpr (E8) x.e = sb[L::EB + 2 * la + 1];
+}
+template <int HD, bool E8>
+__device__ __forceinline__ void clear_tail(Values<HD, E8>& x, int limit, int la) {
 #pragma unroll
-      for (int i = 0; i < TPL; ++i)
-        if (!((seen[t] >> (TPL * la + i)) & 1)) s[t][i / 4][i % 4] = -INFINITY;
-  } else if (limit < L::TOKENS) {  // a tail: tokens past the end may hold anything
-    int lim = limit;
-    asm volatile("" : "+s"(lim));  // (keeps the mask a branch that whole units skip)
+  for (int w = 0; w < 4; ++w) {
+    const uint32_t keep = E8 ? keep_mask<1>(limit - (16 * la + 4 * w)) : keep_mask<2>(limit - (8 * la + 2 * w));
 #pragma unroll
-    for (int t = 0; t < TPW; ++t)
-#pragma unroll
-      for (int i = 0; i < TPL; ++i)
-        if (TPL * la + i >= lim) s[t][i / 4][i % 4] = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const uint32_t keep = E8 ? keep_mask<1>(lim - (TPL * la + 4 * w)) : keep_mask<2>(lim - (TPL * la + 2 * w));
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) vf[nt][w] &= keep;
-      ev[w] &= keep;
-    }
+    for (int nt = 0; nt < HD / 16; ++nt) x.v[nt][w] &= keep;
+    if constexpr (E8) x.e[w] &= keep;
   }
+}
+
+// The scores become weights 2^(s scale - m), and the values are added with them.  weights: of bf16 units.
+template <int HD, bool E8>
+__device__ __forceinline__ void add_values(Rows<HD>& st, f32x4 (&s)[E8 ? 4 : 2], const Values<HD, E8>& x, bf16x8& weights,
+                                           float scale) {
+  constexpr int NT = HD / 16, NH = E8 ? 4 : 2;
 #pragma unroll
-  for (int t = 0; t < TPW; ++t)
-    if (t < ntw) {
-      softmax_step<HD, NH>(st[t], s[t], scale, la);
-      if constexpr (E8)
+  for (int h = 0; h < NH; ++h)
 #pragma unroll
-        for (int i = 0; i < TPL; ++i) s[t][i / 4][i % 4] *= exponent_scale((ev[i / 4] >> (8 * (i % 4))) & 0xffu);
+    for (int r = 0; r < 4; ++r) {
+      s[h][r] = fast_exp2(fmaf(s[h][r], scale, -st.m));
+      st.l += s[h][r];
+      if constexpr (E8) s[h][r] *= exponent_scale((x.e[h] >> (8 * r)) & 0xffu);
     }
+  const bf16x8 p0 = weights8(s, 0);
   if constexpr (E8) {
-    bf16x8 p0[TPW], p1[TPW];
-#pragma unroll
-    for (int t = 0; t < TPW; ++t) {
-      p0[t] = weights8(s[t], 0);
-      p1[t] = weights8(s[t], 2);
-    }
+    const bf16x8 p1 = weights8(s, 2);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      const bf16x8 v0 = from_e4m3(vf[nt][0], vf[nt][1], 1.f), v1 = from_e4m3(vf[nt][2], vf[nt][3], 1.f);
-#pragma unroll
-      for (int t = 0; t < TPW; ++t)
-        if (t < ntw) {
-          st[t].o[nt] = mfma16x16x32_bf16(p0[t], v0, st[t].o[nt]);
-          st[t].o[nt] = mfma16x16x32_bf16(p1[t], v1, st[t].o[nt]);
-        }
+      st.o[nt] = mfma16x16x32_bf16(p0, from_e4m3(x.v[nt][0], x.v[nt][1], 1.f), st.o[nt]);
+      st.o[nt] = mfma16x16x32_bf16(p1, from_e4m3(x.v[nt][2], x.v[nt][3], 1.f), st.o[nt]);
     }
   } else {
+    weights = p0;
 #pragma unroll
-    for (int t = 0; t < TPW; ++t)
-      if (t < ntw) {
-        const bf16x8 p0 = weights8(s[t], 0);
-        if constexpr (NODES) weights[t] = p0;
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-          st[t].o[nt] = mfma16x16x32_bf16(p0, __builtin_bit_cast(bf16x8, vf[nt]), st[t].o[nt]);
-      }
+    for (int nt = 0; nt < NT; ++nt) st.o[nt] = mfma16x16x32_bf16(p0, __builtin_bit_cast(bf16x8, x.v[nt]), st.o[nt]);
   }
 }
 
@@ -354,64 +312,117 @@ __device__ __forceinline__ void add_odd_values(const TreeParams& p, Rows<HD>& st
   }
 }
 
+// The (sequence, split) of work item `item`: first every split that is not its sequence's last,
+// by sequence, then each sequence's last.  So the items that there are come in a row (workgroups past
+// them, which end at once, would otherwise fall on some compute units and spare others) and
+// the uneven ones, which take the nodes too, last.  Every wave searches by itself: 64 sequences
+// at a time, a scan over the lanes.  Batches of more than kScanBatch sequences go in grid order.
+constexpr int kScanBatch = 1024;
+
+__device__ __forceinline__ bool find_item(const TreeParams& p, int item, int lane, int& b, int& s) {
+  const int batch = p.st.batch;
+  if (p.max_splits == 1 || batch > kScanBatch) {
+    b = item / p.max_splits;
+    s = item % p.max_splits;
+    return true;
+  }
+  int base = 0;
+  for (int b0 = 0; b0 < batch; b0 += 64) {
+    const int n = b0 + lane < batch ? clamp_len(p.seq_lens, b0 + lane, p.max_seq_len) : 0;
+    const int full = n > 0 ? (n - 1) / p.split_len : 0;
+    int sum = full;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(sum, o);
+      sum += lane >= o ? v : 0;
+    }
+    const uint64_t past = __ballot(item < base + sum);
+    if (past) {
+      const int at = __ffsll((unsigned long long)past) - 1;
+      b = b0 + at;
+      s = item - (base + __shfl(sum, at) - __shfl(full, at));
+      return true;
+    }
+    base += __shfl(sum, 63);
+  }
+  b = item - base;
+  if (b >= batch) return false;
+  const int n = clamp_len(p.seq_lens, b, p.max_seq_len);
+  s = n > 0 ? (n - 1) / p.split_len : 0;
+  return true;
+}
+
+// Partial results: each tile of 16 rows in the order in which a wave holds it, four values (16 bytes) a
+// lane and side by side: o_part[tile of the split][nt][lane].  bf16 and 8-bit: rows 4 la + r of dim
+// 16 nt + li; fp32: dims 16 nt + 4 la + r of row li.  So both kernels move
+// whole lines.
+__device__ __forceinline__ int64_t tile_of(const TreeParams& p, int b, int g, int s, int row0) {
+  return ((((int64_t)b * p.st.n_kv + g) * p.max_splits + s) * p.r_alloc + row0) >> 4;
+}
+
 __device__ __forceinline__ float lse_of(float m, float l) {
   return l > 0.f || l != l ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
 }
 
-// One workgroup per (group of query tiles, KV head; split; sequence): W waves, an even
-// share of the group's tiles each (at most TPW).  The split's units pass through three LDS stages,
-// loaded two units ahead; every fragment that a wave reads from LDS serves all its tiles.
-// A sequence's last split takes the nodes too.  A sequence of one split is finished here,
-// else its splits leave (m, l) and O for tree_merge.
-template <int HD, bool E8, int W, int TPW>
-__global__ __launch_bounds__(64 * W) void tree_split(const TreeParams p) {
+// One workgroup of four waves per (group of four query tiles, KV head; split; sequence), a tile each.
+// The split's units pass through three LDS stages, loaded two units ahead, a quarter by every
+// wave (a wave without rows too).  A sequence's last split takes the nodes as well, first, while its
+// first units arrive.  A sequence of one split is finished here, else its splits leave (m, l) and O
+// for tree_merge.
+constexpr int kWaves = 4;
+
+template <int HD, bool E8>
+__global__ __launch_bounds__(64 * kWaves, 3) void tree_split(const TreeParams p) {
   using L = Unit<HD, E8>;
-  constexpr int NC = HD / 32, NT = HD / 16, NI = L::NI, NSUB = L::NSUB, U = L::TOKENS;
-  constexpr int PPL = (NI + W - 1) / W, LOADS = PPL + (E8 ? 1 : 0), D = kStages - 1;
-  static_assert(W <= 2 * NI && D * LOADS < 64, "loads in flight");
-  __shared__ u32x4 stage[kStages][L::PIECES];
+  constexpr int NT = HD / 16, NC = HD / 32, NSUB = L::NSUB, U = L::TOKENS, IPG = L::IPG, W = kWaves;
+  constexpr int NS = 3, D = 2;  // LDS stages, units ahead
+  // A wave loads the keys and values of one run of every unit (8-bit: four runs), or its keys or values (two).
+  constexpr int KIND = NSUB == W ? 2 : 1, LOADS = KIND * IPG + (E8 ? 1 : 0);
+  static_assert(KIND * W == 2 * NSUB && D * LOADS < 64, "every run once, and the loads in flight");
+  __shared__ u32x4 stage[NS][L::PIECES];
   __shared__ int blk_ids[2][kIdWin];
   __shared__ int odd_values[W];
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, la = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   __builtin_assume(wave >= 0 && wave < W);
-  const int g = blockIdx.x % p.st.n_kv, qg = blockIdx.x / p.st.n_kv, b = blockIdx.z, s = blockIdx.y;
+  const int g = blockIdx.x % p.st.n_kv, qg = blockIdx.x / p.st.n_kv;
+  int b, s;
+  if (!find_item(p, blockIdx.y + gridDim.y * blockIdx.z, lane, b, s)) return;
+  b = __builtin_amdgcn_readfirstlane(b);
+  s = __builtin_amdgcn_readfirstlane(s);
   const int n = count_of(p, b), rows = n * p.group;
   const int len = clamp_len(p.seq_lens, b, p.max_seq_len);
   const int t0 = s * p.split_len, t1 = min(len, t0 + p.split_len);
-  if ((s > 0 && t0 >= len) || qg * p.n_tiles * 16 >= rows) return;
+  if ((s > 0 && t0 >= len) || qg * W * 16 >= rows) return;
   const bool whole = len <= p.split_len, last = t1 == len;
-  const int tb = wave * p.n_tiles / W, ntw = TPW == 1 ? 1 : (wave + 1) * p.n_tiles / W - tb;
-  const int row0 = (qg * p.n_tiles + tb) * 16;
+  const int row0 = (qg * W + wave) * 16;
+  const bool active = row0 < rows;
 
-  Rows<HD> st[TPW];
+  Rows<HD> st;
+  const int row = min(row0 + li, rows - 1), node = row / p.group, head = g * p.group + row % p.group;
+  {
+    const bf16* q = (const bf16*)p.q.data + ((int64_t)b * p.nodes + node) * p.q.row + (int64_t)head * p.q.head;
 #pragma unroll
-  for (int t = 0; t < TPW; ++t) {
-    const int row = min(row0 + 16 * t + li, rows - 1);
-    const bf16* q = (const bf16*)p.q.data + ((int64_t)b * p.nodes + row / p.group) * p.q.row +
-                    (int64_t)(g * p.group + row % p.group) * p.q.head;
-#pragma unroll
-    for (int c = 0; c < NC; ++c) st[t].q[c] = __builtin_bit_cast(bf16x8, row8(q + 8 * (la * NC + c), p.q_vec));
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) st[t].o[nt] = f32x4{0.f, 0.f, 0.f, 0.f};
-    st[t].m = kNegBig;
-    st[t].l = 0.f;
+    for (int c = 0; c < NC; ++c) st.q[c] = __builtin_bit_cast(bf16x8, row8(q + 8 * (la * NC + c), p.q_vec));
   }
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) st.o[nt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  st.m = kNegBig;
+  st.l = 0.f;
 
   const StoreArg& c = p.st;
   constexpr int ESZ = E8 ? 1 : 2;
-  const char* kbase = (const char*)c.k + g * c.k_sh * ESZ;
-  const char* vbase = (const char*)c.v + g * c.v_sh * ESZ;
   const int bs = 1 << c.bs_log2, nunits = (t1 - t0 + U - 1) / U, lastu = nunits - 1;
   const int lb0 = t0 >> c.bs_log2, nlb = t1 > t0 ? ((t1 - 1) >> c.bs_log2) - lb0 + 1 : 0;
   const int* bt_row = c.block_table ? c.block_table + (int64_t)b * c.mbps + lb0 : nullptr;
   // The first two windows of block ids and the first nodes are under way together.
-  constexpr int IDS = 2 * kIdWin / (64 * W) + (2 * kIdWin % (64 * W) != 0);
+  constexpr int IDS = 2 * kIdWin / (64 * W);
+  static_assert(IDS * 64 * W == 2 * kIdWin, "ids per thread");
   int ids[IDS];
 #pragma unroll
   for (int j = 0; j < IDS; ++j) {
     const int i = j * 64 * W + tid;
-    ids[j] = bt_row && i < nlb ? bt_row[i] : 0;
+    ids[j] = !bt_row ? b * c.mbps + lb0 + i : i < nlb ? bt_row[i] : 0;
   }
   if (last) {
     const bool odd = stage_nodes<HD, W>(p, stage[D], b, g, 0, n, tid);
@@ -419,84 +430,84 @@ __global__ __launch_bounds__(64 * W) void tree_split(const TreeParams p) {
     if (lane == 0) odd_values[wave] = any;
   }
 #pragma unroll
-  for (int j = 0; j < IDS; ++j) {
-    const int i = j * 64 * W + tid;
-    if (i < 2 * kIdWin) blk_ids[i / kIdWin][i % kIdWin] = ids[j];
-  }
+  for (int j = 0; j < IDS; ++j) (&blk_ids[0][0])[j * 64 * W + tid] = ids[j];
   auto load_window = [&](int w) __attribute__((always_inline)) {
-    for (int j = wave; j < kIdWin / 64; j += W)  // past the end: the last id again
-      ld4_to_lds(bt_row + min(w * kIdWin + j * 64 + lane, nlb - 1), &blk_ids[w & 1][j * 64]);
+    for (int j = wave; j < kIdWin / 64; j += W) {
+      const int i = min(w * kIdWin + j * 64 + lane, nlb - 1);  // past the end: the last id again
+      if (bt_row) ld4_to_lds(bt_row + i, &blk_ids[w & 1][j * 64]);
+      else blk_ids[w & 1][j * 64 + lane] = b * c.mbps + lb0 + i;
+    }
   };
-  uint32_t lane_off[PPL];
-  int gsel[PPL], lds_piece[PPL];
-#pragma unroll
-  for (int j = 0; j < PPL; ++j) {
-    const int slot = (j * W + wave) % NI;  // (a wave count that does not divide NI loads a few twice)
-    gsel[j] = L::IPG % W == 0 ? j * W / L::IPG : slot / L::IPG;
-    lds_piece[j] = L::group_base(gsel[j]) + (slot % L::IPG) * 64;
-    const int q = (slot % L::IPG) * 64 + lane;
-    lane_off[j] = gsel[j] < NSUB ? L::key_off(q, bs) : L::value_off(q, bs);
-  }
-  const int er = (lane >> 2) & 3;  // exponents: lanes 0..15 the keys', 16..31 the values', then both again
+  // This wave's run of a unit, and what it loads of it: first kind 0 keys, 1 values.
+  const int run = wave * NSUB / W, kind0 = KIND == 1 ? wave & 1 : 0;
+  uint32_t lane_off[KIND][IPG];
+  const char* kind_base[KIND];  // a run's place: kind_base + block * block_step + (slot << slot_shift)
+  uint64_t block_step[KIND];
+  int slot_shift[KIND], piece0[KIND];
   // Loads are streaming (read once by this launch), unless another query group reads the
-  // same blocks, or a unit takes less than its 64 bytes of a dim's row of values.
-  const bool k_stream = p.n_qgroups == 1, v_stream = k_stream && bs * ESZ <= 64;
-  auto issue = [&](int u, int buf) __attribute__((always_inline)) {
-    int64_t blk[NSUB];
-    int slot[NSUB];
+  // same blocks, or a unit takes less than 64 bytes of a dim's row of values.
+  bool stream[KIND];
 #pragma unroll
-    for (int r = 0; r < NSUB; ++r) {
-      int t = t0 + U * u + 16 * r;
-      t = t < t1 ? t : t0 + U * u;  // a run past the end reads the unit's first again
-      const int rel = (t >> c.bs_log2) - lb0;
-      slot[r] = t & (bs - 1);
-      if (bt_row) blk[r] = __builtin_amdgcn_readfirstlane(blk_ids[((unsigned)rel / kIdWin) & 1][(unsigned)rel % kIdWin]);
-      else blk[r] = (int64_t)b * c.mbps + lb0 + rel;
+  for (int k = 0; k < KIND; ++k) {
+    const bool v = kind0 + k;
+#pragma unroll
+    for (int j = 0; j < IPG; ++j) lane_off[k][j] = v ? L::value_off(64 * j + lane, bs) : L::key_off(64 * j + lane, bs);
+    kind_base[k] = v ? (const char*)c.v + g * c.v_sh * ESZ : (const char*)c.k + g * c.k_sh * ESZ;
+    block_step[k] = (uint64_t)(v ? c.v_sb : c.k_sb) * ESZ;
+    slot_shift[k] = v ? (E8 ? 0 : 1) : 4;
+    piece0[k] = v ? L::VB + run * L::SUB : run * L::KP;
+    stream[k] = p.n_qgroups == 1 && (!v || bs * ESZ <= 64);
+  }
+  const uint8_t* exp_base = lane & 4 ? c.v_exp : c.k_exp;  // 8-bit: lanes 0..3 the keys' exponents, 4..7 the values'
+  const uint32_t blocks = (uint32_t)(c.num_blocks < 0xffffffffll ? c.num_blocks : 0xffffffffll);
+  // The next unit to issue: its number, the first token of this wave's run, and that run's block id,
+  // read from LDS one unit ahead.  A run past the end reads the unit's first again.
+  int next_u = 0, next_t = 0, next_id = 0;
+  // When the ids read enter window w >= 1 (block ids from w * kIdWin), window w + 1 replaces w - 1,
+  // which no later unit reads; kIdWin blocks later it has long landed.  (Units start at multiples
+  // of 64 tokens, so no unit lies in two windows.)
+  int window_end = kIdWin;
+  auto look_ahead = [&]() __attribute__((always_inline)) {
+    const int first = t0 + U * min(next_u, lastu);
+    next_t = first + 16 * run < t1 ? first + 16 * run : first;
+    const int rel = (next_t >> c.bs_log2) - lb0;
+    next_id = (&blk_ids[0][0])[rel & (2 * kIdWin - 1)];
+    if (rel >= window_end) {
+      window_end += kIdWin;
+      if (window_end < nlb) load_window(window_end / kIdWin);
     }
-    const char *kr[NSUB], *vr[NSUB];
+  };
+  auto issue = [&](int buf) __attribute__((always_inline)) {
+    uint32_t blk = (uint32_t)__builtin_amdgcn_readfirstlane(next_id);
+    blk = blk < blocks ? blk : 0;
+    const uint32_t slot = next_t & (bs - 1);
 #pragma unroll
-    for (int r = 0; r < NSUB; ++r) {
-      blk[r] = blk[r] >= 0 && blk[r] < c.num_blocks ? blk[r] : 0;
-      kr[r] = kbase + blk[r] * c.k_sb * ESZ + slot[r] * 16;
-      vr[r] = vbase + blk[r] * c.v_sb * ESZ + slot[r] * ESZ;
-    }
+    for (int k = 0; k < KIND; ++k) {
+      const char* base = kind_base[k] + blk * block_step[k] + (slot << slot_shift[k]);
+      u32x4* to = &stage[buf][piece0[k]];
+      if (stream[k]) {
 #pragma unroll
-    for (int j = 0; j < PPL; ++j) {
-      const char* base = kr[0];
+        for (int j = 0; j < IPG; ++j) ld16_to_lds(base, lane_off[k][j], to + 64 * j);
+      } else {
 #pragma unroll
-      for (int r = 1; r < NSUB; ++r) base = gsel[j] == r ? kr[r] : base;
-#pragma unroll
-      for (int r = 0; r < NSUB; ++r) base = gsel[j] == NSUB + r ? vr[r] : base;
-      if (gsel[j] < NSUB ? k_stream : v_stream) ld16_to_lds(base, lane_off[j], &stage[buf][lds_piece[j]]);
-      else ld16_to_lds<false>(base, lane_off[j], &stage[buf][lds_piece[j]]);
-    }
-    if constexpr (E8) {
-      int64_t eb = blk[0];
-      int es = slot[0];
-#pragma unroll
-      for (int r = 1; r < NSUB; ++r) {
-        eb = er == r ? blk[r] : eb;
-        es = er == r ? slot[r] : es;
+        for (int j = 0; j < IPG; ++j) ld16_to_lds<false>(base, lane_off[k][j], to + 64 * j);
       }
-      const uint8_t* e = lane & 16 ? c.v_exp : c.k_exp;
-      ld4_to_lds(e + eb * c.e_sb + g * c.e_sh + es + 4 * (lane & 3), &stage[buf][L::EB]);
     }
+    if constexpr (E8)
+      if (lane < 8) ld4_to_lds(exp_base + blk * (uint64_t)c.e_sb + g * c.e_sh + slot + 4 * (lane & 3), &stage[buf][L::EB + 2 * run]);
+    ++next_u;
+    look_ahead();
   };
-  // entering window w when issuing unit v: window w + 1 replaces w - 1, which no later unit reads
-  auto next_window = [&](int v) __attribute__((always_inline)) {
-    const int w = (((t0 + U * v) >> c.bs_log2) - lb0) / kIdWin;
-    const int wp = (((t0 + U * (v - 1)) >> c.bs_log2) - lb0) / kIdWin;
-    if (bt_row && w != wp && (w + 1) * kIdWin < nlb) load_window(w + 1);
-  };
-  uint32_t seen[TPW];
-  bf16x8 weights[TPW];
+  bf16x8 weights;
   // nothing that the compiler counts stays in flight past this point
   wait_vmcnt<0>();
   lds_barrier();
-#pragma unroll
-  for (int v = 0; v < D; ++v)
-    if (v <= lastu) issue(v, v);
-  if (last)  // the nodes, from the stage that unit D will take, while the first units arrive
+  if (nunits > 0) {
+    look_ahead();
+    issue(0);
+    if (lastu > 0) issue(1);
+  }
+  if (last)  // the nodes, from the stage that unit D will take
     for (int u = 0; 32 * u < n; ++u) {
       if (u > 0) {
         lds_barrier();
@@ -505,97 +516,158 @@ __global__ __launch_bounds__(64 * W) void tree_split(const TreeParams p) {
         if (lane == 0) odd_values[wave] = any;
         lds_barrier();
       }
+      if (!active) continue;
+      const uint32_t seen = seen_word(p, b, node, u, n);
+      f32x4 sc[2];
+      Values<HD, false> x;
+      unit_scores<HD, false>(st, sc, stage[D], li, la);
+      read_values(x, stage[D], li, la);
 #pragma unroll
-      for (int t = 0; t < TPW; ++t) seen[t] = seen_word(p, b, min(row0 + 16 * t + li, rows - 1) / p.group, u, n);
-      staged_unit<HD, false, TPW, true>(st, ntw, stage[D], 32, seen, weights, p.scale_log2, li, la);
+      for (int i = 0; i < 8; ++i)
+        if (!((seen >> (8 * la + i)) & 1)) sc[i / 4][i % 4] = -INFINITY;
+      raise_maximum(st, sc, p.scale_log2, la);
+      add_values<HD, false>(st, sc, x, weights, p.scale_log2);
       bool odd = false;
 #pragma unroll
       for (int w = 0; w < W; ++w) odd |= odd_values[w] != 0;
-      if (odd)
-#pragma unroll
-        for (int t = 0; t < TPW; ++t)
-          if (t < ntw) add_odd_values<HD>(p, st[t], weights[t], b, g, u, n, li, la);
+      if (odd) add_odd_values<HD>(p, st, weights, b, g, u, n, li, la);
     }
   int buf = 0;
   for (int u = 0; u < nunits; ++u) {
-    // this wave's loads of unit u have landed; after the barrier everyone's have, and all are past unit u - 1
-    wait_units_le<LOADS, D - 1>(min(u + D - 1, lastu) - u);
+    // this wave's loads of unit u have landed; after the barrier everyone's have, and all are past
+    // unit u - 1, whose stage unit u + D takes
+    if (u < lastu) wait_vmcnt<LOADS>();
+    else wait_vmcnt<0>();
     lds_barrier();
-    if (u + D <= lastu) {
-      issue(u + D, buf == 0 ? kStages - 1 : buf - 1);
-      next_window(u + D);
+    if (u + D <= lastu) issue(buf == 0 ? NS - 1 : buf - 1);
+    const u32x4* sb = stage[buf];
+    buf = buf == NS - 1 ? 0 : buf + 1;
+    if (!active) continue;
+    f32x4 sc[E8 ? 4 : 2];
+    Values<HD, E8> x;
+    unit_scores<HD, E8>(st, sc, sb, li, la);
+    // values are read once the scores' products are issued, into registers the keys held
+    __builtin_amdgcn_sched_barrier(0);
+    read_values(x, sb, li, la);
+    if (u == lastu) {
+      int limit = t1 - (t0 + U * u);
+      asm volatile("" : "+s"(limit));  // (keeps the masks a branch that whole units skip)
+      mask_tail(sc, limit, la);
+      clear_tail(x, limit, la);
     }
-    staged_unit<HD, E8, TPW, false>(st, ntw, stage[buf], t1 - (t0 + U * u), seen, weights, p.scale_log2, li, la);
-    buf = buf == kStages - 1 ? 0 : buf + 1;
+    raise_maximum(st, sc, p.scale_log2, la);
+    add_values<HD, E8>(st, sc, x, weights, p.scale_log2);
   }
+
+  if (!active) return;
+  float l = st.l;
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+  if (whole) {
+    if (p.lse && la == 0 && row0 + li < rows) p.lse[((int64_t)b * p.nodes + node) * (p.st.n_kv * p.group) + head] = lse_of(st.m, l);
 #pragma unroll
-  for (int t = 0; t < TPW; ++t) {
-    const int r0 = row0 + 16 * t;
-    if (t >= ntw || r0 >= rows) continue;
-    float l = st[t].l;
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
-    if (whole) {
-      const int row = r0 + li;
-      if (p.lse && la == 0 && row < rows)
-        p.lse[((int64_t)b * p.nodes + row / p.group) * (p.st.n_kv * p.group) + g * p.group + row % p.group] = lse_of(st[t].m, l);
+    for (int r = 0; r < 4; ++r) {
+      const float lr = __shfl(l, 4 * la + r);
+      const float inv = lr == 0.f ? 0.f : 1.0f / lr;
+      const int orow = row0 + 4 * la + r;
+      if (orow >= rows) continue;
+      bf16* o = (bf16*)p.out.data + ((int64_t)b * p.nodes + orow / p.group) * p.out.row +
+                (int64_t)(g * p.group + orow % p.group) * p.out.head;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float lr = __shfl(l, 4 * la + r);
-        const float inv = lr == 0.f ? 0.f : 1.0f / lr;
-        const int orow = r0 + 4 * la + r;
-        if (orow >= rows) continue;
-        bf16* o = (bf16*)p.out.data + ((int64_t)b * p.nodes + orow / p.group) * p.out.row +
-                  (int64_t)(g * p.group + orow % p.group) * p.out.head;
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) o[16 * nt + li] = (bf16)(st[t].o[nt][r] * inv);
-      }
-    } else {
-      const int64_t prow = (((int64_t)b * p.st.n_kv + g) * p.max_splits + s) * p.r_alloc + r0;
-      if (la == 0) p.ml_part[prow + li] = make_float2(st[t].m, l);
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) p.o_part[(prow + 4 * la + r) * HD + 16 * nt + li] = st[t].o[nt][r];
+      for (int nt = 0; nt < NT; ++nt) o[16 * nt + li] = (bf16)(st.o[nt][r] * inv);
     }
+  } else {
+    const int64_t tile = tile_of(p, b, g, s, row0);
+    if (la == 0) p.ml_part[16 * tile + li] = make_float2(st.m, l);
+    if (row0 + 4 * la < rows)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) ((f32x4*)p.o_part)[(tile * NT + nt) * 64 + lane] = st.o[nt];
   }
 }
 
-// Joins the splits of the sequences that have several: one wave per query row, its lanes
-// along the dims, every split's O weighted by 2^(m - the largest m).
-template <int HD, typename T>
+// Joins the splits of the sequences that have several: one workgroup per tile, every split's O
+// weighted by 2^(m - the largest m).  The 16 rows' weights of up to 32 splits at a time are found by
+// all threads and shared through LDS.
+template <int HD, typename T, bool F32>
 __global__ __launch_bounds__(256) void tree_merge(const TreeParams p) {
-  constexpr int V = HD / 64;
-  const int lane = threadIdx.x & 63, g = blockIdx.y, b = blockIdx.z;
-  const int row = 4 * blockIdx.x + (threadIdx.x >> 6);
-  const int len = clamp_len(p.seq_lens, b, p.max_seq_len);
-  if (len <= p.split_len || row >= count_of(p, b) * p.group) return;
+  constexpr int PER = HD / 64, CH = 32;
+  __shared__ __align__(16) float wsh[CH][16];
+  __shared__ float red[16][17];
+  const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, la = lane >> 4;
+  const int row0 = 16 * blockIdx.x, g = blockIdx.y, b = blockIdx.z;
+  const int len = clamp_len(p.seq_lens, b, p.max_seq_len), rows = count_of(p, b) * p.group;
+  if (len <= p.split_len || row0 >= rows) return;
   const int ns = (len + p.split_len - 1) / p.split_len;
-  const int64_t base = ((int64_t)b * p.st.n_kv + g) * p.max_splits * p.r_alloc + row;
-  float m = kNegBig;
-  for (int s = lane; s < ns; s += 64) m = fmaxf(m, p.ml_part[base + (int64_t)s * p.r_alloc].x);
+  const int r = tid & 15, c = tid >> 4;
+  const float2* ml = p.ml_part + 16 * tile_of(p, b, g, 0, row0) + r;
+  float m = kNegBig, l = 0.f;
+  for (int s = c; s < ns; s += 16) m = fmaxf(m, ml[(int64_t)s * p.r_alloc].x);
+  red[r][c] = m;
+  __syncthreads();
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
-  float l = 0.f, acc[V] = {};
+  for (int i = 0; i < 16; ++i) m = fmaxf(m, red[r][i]);
+  const bool mine = F32 ? row0 + li < rows : row0 + 4 * la < rows;  // whether the lane's values hold a row
+  const f32x4* o = (const f32x4*)p.o_part + tile_of(p, b, g, 0, row0) * (HD * 4) + tid;
+  const int64_t o_split = (int64_t)p.r_alloc / 16 * (HD * 4);
+  f32x4 acc[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int s0 = 0; s0 < ns; s0 += CH) {
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < CH; j += 16) {
+      const int s = s0 + c + j;
+      float w = 0.f;
+      if (s < ns) {
+        const float2 x = ml[(int64_t)s * p.r_alloc];
+        w = fast_exp2(x.x - m);
+        l += w * x.y;
+      }
+      wsh[c + j][r] = w;
+    }
+    __syncthreads();
+    if (!mine) continue;
+    const int k1 = min(CH, ns - s0);
 #pragma unroll 4
-  for (int s = 0; s < ns; ++s) {
-    const int64_t at = base + (int64_t)s * p.r_alloc;
-    const float2 ml = p.ml_part[at];
-    const float w = fast_exp2(ml.x - m);
-    l += w * ml.y;
+    for (int k = 0; k < k1; ++k)
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const float x = p.o_part[at * HD + V * lane + i];
-      acc[i] += w * x;
+      for (int i = 0; i < PER; ++i) {
+        const f32x4 x = o[(s0 + k) * o_split + 256 * i];
+        if (F32) acc[i] += x * wsh[k][li];
+        else acc[i] += x * *reinterpret_cast<const f32x4*>(&wsh[k][4 * la]);
+      }
+  }
+  __syncthreads();
+  red[r][c] = l;
+  __syncthreads();
+  l = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) l += red[r][i];
+  __syncthreads();
+  if (c == 0) {
+    red[r][16] = l == 0.f ? 0.f : 1.0f / l;
+    const int row = row0 + r;
+    if (p.lse && row < rows)
+      p.lse[((int64_t)b * p.nodes + row / p.group) * (p.st.n_kv * p.group) + g * p.group + row % p.group] = lse_of(m, l);
+  }
+  __syncthreads();
+  if (!mine) return;
+#pragma unroll
+  for (int e = 0; e < (F32 ? 1 : 4); ++e) {
+    const int rr = F32 ? li : 4 * la + e, row = row0 + rr;
+    if (row >= rows) continue;
+    T* out = (T*)p.out.data + ((int64_t)b * p.nodes + row / p.group) * p.out.row + (int64_t)(g * p.group + row % p.group) * p.out.head;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int nt = (256 * i + tid) >> 6;
+      if (F32) {
+#pragma unroll
+        for (int d = 0; d < 4; ++d) out[16 * nt + 4 * la + d] = from_f32<T>(acc[i][d] * red[rr][16]);
+      } else {
+        out[16 * nt + li] = from_f32<T>(acc[i][e] * red[rr][16]);
+      }
     }
   }
-  const int head = g * p.group + row % p.group;
-  const int64_t node = (int64_t)b * p.nodes + row / p.group;
-  if (p.lse && lane == 0) p.lse[node * (p.st.n_kv * p.group) + head] = lse_of(m, l);
-  const float inv = l == 0.f ? 0.f : 1.0f / l;
-  T* o = (T*)p.out.data + node * p.out.row + (int64_t)head * p.out.head;
-#pragma unroll
-  for (int i = 0; i < V; ++i) o[V * lane + i] = from_f32<T>(acc[i] * inv);
 }
 
 // ---------------------------------------------------------------- fp32
@@ -614,7 +686,11 @@ __global__ __launch_bounds__(64 * kF32Waves) void tree_split_f32(const TreeParam
   __shared__ float2 mlsh[NW][64];
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, la = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int g = blockIdx.x % p.st.n_kv, row0 = 16 * (blockIdx.x / p.st.n_kv), b = blockIdx.z, s = blockIdx.y;
+  const int g = blockIdx.x % p.st.n_kv, row0 = 16 * (blockIdx.x / p.st.n_kv);
+  int b, s;
+  if (!find_item(p, blockIdx.y + gridDim.y * blockIdx.z, lane, b, s)) return;
+  b = __builtin_amdgcn_readfirstlane(b);
+  s = __builtin_amdgcn_readfirstlane(s);
   const int n = count_of(p, b), rows = n * p.group;
   const int len = clamp_len(p.seq_lens, b, p.max_seq_len);
   const int begin = s * p.split_len, end = min(len, begin + p.split_len);
@@ -745,23 +821,10 @@ __global__ __launch_bounds__(64 * kF32Waves) void tree_split_f32(const TreeParam
 #pragma unroll
     for (int r = 0; r < 4; ++r) op[r] = x[r] * inv;
   } else {
-    const int64_t prow = (((int64_t)b * p.st.n_kv + g) * p.max_splits + s) * p.r_alloc + row0 + li;
-    if (wave == 0 && la == 0) p.ml_part[prow] = make_float2(mg, lg);
-    *reinterpret_cast<f32x4*>(p.o_part + prow * HD + 16 * wave + 4 * la) = x;
+    const int64_t tile = tile_of(p, b, g, s, row0);
+    if (wave == 0 && la == 0) p.ml_part[16 * tile + li] = make_float2(mg, lg);
+    ((f32x4*)p.o_part)[(tile * NJ + wave) * 64 + lane] = x;
   }
-}
-
-template <int HD, bool E8>
-hipError_t split_typed(const TreeParams& p, dim3 grid, int waves, int tpw, hipStream_t s) {
-#define SP_TREE_CASE(W_, TPW_)                                                            \
-  if (waves == W_ && tpw == TPW_) {                                                       \
-    hipLaunchKernelGGL((tree_split<HD, E8, W_, TPW_>), grid, dim3(64 * W_), 0, s, p);     \
-    return hipGetLastError();                                                             \
-  }
-  SP_TREE_CASE(1, 1) SP_TREE_CASE(2, 1) SP_TREE_CASE(3, 1) SP_TREE_CASE(4, 1)
-  SP_TREE_CASE(4, 2) SP_TREE_CASE(4, 3) SP_TREE_CASE(4, 4)
-#undef SP_TREE_CASE
-  return hipErrorInvalidValue;
 }
 
 }  // namespace
@@ -776,22 +839,25 @@ hipError_t launch_tree(const TreeParams& p, int storage, int hd, hipStream_t s) 
     else hipLaunchKernelGGL((tree_split_f32<64>), grid, block, 0, s, p);
     e = hipGetLastError();
   } else {
-    const int tpw = (p.n_tiles + p.waves - 1) / p.waves;
-    if (p.split_len % 64 || p.n_qgroups * p.n_tiles * 16 > p.r_alloc || (tpw == 1 && p.n_tiles != p.waves))
-      return hipErrorInvalidValue;
-    const dim3 grid(p.st.n_kv * p.n_qgroups, p.max_splits, p.st.batch);
-    const bool e8 = storage == SP_E4M3;
-    e = hd == 128 ? (e8 ? split_typed<128, true>(p, grid, p.waves, tpw, s) : split_typed<128, false>(p, grid, p.waves, tpw, s))
-                  : (e8 ? split_typed<64, true>(p, grid, p.waves, tpw, s) : split_typed<64, false>(p, grid, p.waves, tpw, s));
+    if (p.split_len % 64 || p.r_alloc < rows || p.r_alloc != p.n_qgroups * 16 * kWaves) return hipErrorInvalidValue;
+    const dim3 grid(p.st.n_kv * p.n_qgroups, p.max_splits, p.st.batch), block(64 * kWaves);
+    if (storage == SP_E4M3) {
+      if (hd == 128) hipLaunchKernelGGL((tree_split<128, true>), grid, block, 0, s, p);
+      else hipLaunchKernelGGL((tree_split<64, true>), grid, block, 0, s, p);
+    } else {
+      if (hd == 128) hipLaunchKernelGGL((tree_split<128, false>), grid, block, 0, s, p);
+      else hipLaunchKernelGGL((tree_split<64, false>), grid, block, 0, s, p);
+    }
+    e = hipGetLastError();
   }
   if (e != hipSuccess || p.max_splits == 1) return e;
-  const dim3 mgrid((rows + 3) / 4, p.st.n_kv, p.st.batch), block(256);
+  const dim3 mgrid((rows + 15) / 16, p.st.n_kv, p.st.batch), block(256);
   if (storage == SP_F32) {
-    if (hd == 128) hipLaunchKernelGGL((tree_merge<128, float>), mgrid, block, 0, s, p);
-    else hipLaunchKernelGGL((tree_merge<64, float>), mgrid, block, 0, s, p);
+    if (hd == 128) hipLaunchKernelGGL((tree_merge<128, float, true>), mgrid, block, 0, s, p);
+    else hipLaunchKernelGGL((tree_merge<64, float, true>), mgrid, block, 0, s, p);
   } else {
-    if (hd == 128) hipLaunchKernelGGL((tree_merge<128, bf16>), mgrid, block, 0, s, p);
-    else hipLaunchKernelGGL((tree_merge<64, bf16>), mgrid, block, 0, s, p);
+    if (hd == 128) hipLaunchKernelGGL((tree_merge<128, bf16, false>), mgrid, block, 0, s, p);
+    else hipLaunchKernelGGL((tree_merge<64, bf16, false>), mgrid, block, 0, s, p);
   }
   return hipGetLastError();
 }
