@@ -92,39 +92,77 @@ __device__ __forceinline__ PairOf pair_of(int d, int rotary_dim, int layout) {
 }
 
 // ---------------------------------------------------------------- rotary
-// One workgroup per row: the row's cosines and sines once into LDS, then every value
-// of every head.  A pair is read and written by one lane, so the output may be the
-// input.
-template <typename T>
+// One workgroup per R rows: their cosines and sines once into LDS (fp64 angles), then each thread
+// takes the same piece of every row, so that R rows' loads are under way together.  A pair
+// is read and written by one lane, so the output may be the input.  Pieces (V values, 16
+// bytes, where every head is aligned so): of interleaved heads V values of a head; of half
+// heads V pairs, or V values that stay.  Else single pairs and values (kScalar).
+// 16384 rows of 48 heads (half of each rotated, bf16, 403 MB): see launch_rotary.
+enum RotaryMode { kScalar, kHalf, kInterleaved };
+constexpr int kRotaryRows = 4;
+
+template <typename T, int MODE, int R>
 __global__ __launch_bounds__(256) void rotary_rows(const RotaryParams p) {
-  __shared__ float cs[64], sn[64];
-  const int row = blockIdx.x, hd = p.rot.head_dim, rd = p.rot.rotary_dim, half = rd >> 1;
-  const int pos = p.positions[row];
-  if (pos < 0) return;
-  if ((int)threadIdx.x < half) {
+  constexpr int V = MODE == kScalar ? 1 : 16 / (int)sizeof(T);
+  typedef T Piece __attribute__((ext_vector_type(V)));
+  __shared__ __align__(16) float cs[R][64], sn[R][64];
+  __shared__ int live[R];
+  const int row0 = blockIdx.x * R, hd = p.rot.head_dim, rd = p.rot.rotary_dim, half = rd >> 1;
+  if ((int)threadIdx.x < R) live[threadIdx.x] = row0 + (int)threadIdx.x < p.n_rows && p.positions[row0 + threadIdx.x] >= 0;
+  for (int e = threadIdx.x; e < R * half; e += 256) {
+    const int r = e / half, i = e - r * half;
+    if (row0 + r >= p.n_rows) break;
     float c, s;
-    cos_sin_turns((double)pos * p.rot.turns[threadIdx.x], c, s);
-    cs[threadIdx.x] = c * p.rot.scale;
-    sn[threadIdx.x] = (p.transpose ? -s : s) * p.rot.scale;
+    cos_sin_turns((double)p.positions[row0 + r] * p.rot.turns[i], c, s);
+    cs[r][i] = c * p.rot.scale;
+    sn[r][i] = (p.transpose ? -s : s) * p.rot.scale;
   }
   __syncthreads();
-  const int items = half + hd - rd;  // pairs, then the values that stay
-  for (int a = 0; a < 2; ++a) {
-    const T* x = (const T*)p.in[a].data + (int64_t)row * p.in[a].row;
-    T* y = (T*)p.out[a].data + (int64_t)row * p.out[a].row;
-    for (int e = threadIdx.x; e < p.n_heads[a] * items; e += 256) {
-      const int h = e / items, i = e % items;
-      const T* xh = x + h * p.in[a].head;
-      T* yh = y + h * p.out[a].head;
-      if (i < half) {
-        const int d0 = p.rot.layout == SP_ROTARY_INTERLEAVED ? 2 * i : i;
-        const int d1 = pair_of(d0, rd, p.rot.layout).other;
-        const float x0 = to_f32(xh[d0]), x1 = to_f32(xh[d1]);
-        yh[d0] = from_f32<T>(x0 * cs[i] - x1 * sn[i]);
-        yh[d1] = from_f32<T>(x1 * cs[i] + x0 * sn[i]);
-      } else {
-        yh[rd + i - half] = xh[rd + i - half];
+  const bool inter = MODE == kInterleaved || (MODE == kScalar && p.rot.layout == SP_ROTARY_INTERLEAVED);
+  // pieces of a head: those that turn, then those that stay
+  const int turn = MODE == kInterleaved ? (rd + V - 1) / V : half / V;
+  const int stay0 = MODE == kInterleaved ? turn * V : rd, items = turn + (hd - stay0) / V;
+  for (int e = threadIdx.x; e < (p.n_heads[0] + p.n_heads[1]) * items; e += 256) {
+    const int hh = e / items, i = e - hh * items;
+    const int a = hh >= p.n_heads[0] ? 1 : 0, h = a ? hh - p.n_heads[0] : hh;
+    const T* x = (const T*)p.in[a].data + (int64_t)row0 * p.in[a].row + h * p.in[a].head;
+    T* y = (T*)p.out[a].data + (int64_t)row0 * p.out[a].row + h * p.out[a].head;
+    // first value of the piece, and of its pairs' other members
+    const int d0 = i >= turn ? stay0 + (i - turn) * V : inter ? i * (MODE == kScalar ? 2 : V) : i * V;
+    const int d1 = MODE == kScalar && inter ? d0 + 1 : d0 + half;
+    const bool second = MODE != kInterleaved && i < turn;
+    Piece u[R], w[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      if (live[r]) {
+        u[r] = *reinterpret_cast<const Piece*>(x + r * p.in[a].row + d0);
+        if (second) w[r] = *reinterpret_cast<const Piece*>(x + r * p.in[a].row + d1);
       }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (!live[r]) continue;
+      if (i < turn) {
+        if constexpr (MODE == kInterleaved) {
+#pragma unroll
+          for (int j = 0; j < V / 2; ++j) {
+            const int pair = i * (V / 2) + j;
+            if (pair >= half) break;  // (the last piece of a rotary_dim that V does not divide)
+            const float x0 = to_f32(u[r][2 * j]), x1 = to_f32(u[r][2 * j + 1]);
+            u[r][2 * j] = from_f32<T>(x0 * cs[r][pair] - x1 * sn[r][pair]);
+            u[r][2 * j + 1] = from_f32<T>(x1 * cs[r][pair] + x0 * sn[r][pair]);
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < V; ++j) {
+            const int pair = i * V + j;
+            const float x0 = to_f32(u[r][j]), x1 = to_f32(w[r][j]);
+            u[r][j] = from_f32<T>(x0 * cs[r][pair] - x1 * sn[r][pair]);
+            w[r][j] = from_f32<T>(x1 * cs[r][pair] + x0 * sn[r][pair]);
+          }
+        }
+      }
+      *reinterpret_cast<Piece*>(y + r * p.out[a].row + d0) = u[r];
+      if (second) *reinterpret_cast<Piece*>(y + r * p.out[a].row + d1) = w[r];
     }
   }
 }
@@ -189,11 +227,12 @@ __device__ __forceinline__ void pack(const float (&x)[16], Stored<TS>& out, int&
 }
 
 // ---------------------------------------------------------------- write
-// One workgroup per (tile of 64 rows, heads_per_wg KV heads).  Keys go straight from
-// registers: 16 values are one, two or four pieces of the paged layout, and eight rows of
-// a wave that follow one another in a block make 128 consecutive bytes of each piece.
-// Values lie dim-major in the cache, so they pass through LDS: where the rows of a tile
-// fill an aligned group of 16 bytes' worth of slots (a "group": 4, 8 or 16 rows that
+// Workgroups per tile of 64 rows: one for the values of each KV head, one for the keys of every
+// heads_per_wg heads.  Keys go straight from registers: 16 values are one, two or four
+// pieces of the paged layout, and eight rows of a wave that follow one another in a block make
+// 128 consecutive bytes of each piece; their angles' cosines and sines are found once for all
+// of the workgroup's heads.  Values lie dim-major in the cache, so they pass through LDS: where the rows of
+// a tile fill an aligned group of 16 bytes' worth of slots (a "group": 4, 8 or 16 rows that
 // follow one another), each dim of it is one 16-byte store; what is left, at a run's
 // ends or with scattered rows, is stored value by value.
 constexpr int kTile = 64;
@@ -240,98 +279,130 @@ __device__ __forceinline__ void plan_tile(const CacheParams& p, int row0, TilePl
   }
 }
 
-template <typename TS, typename TI, int HD, bool ROT>
+enum KeyRotation { kNoRotation, kAnyRotation, kHalf16 };  // kHalf16: half layout, rotary_dim / 2 a multiple of 16
+
+template <typename TS, typename TI, int HD, int ROT>
 __global__ __launch_bounds__(256) void cache_write(const CacheParams p, const sp_rotary rot) {
   constexpr int LR = HD / 16, RP = 256 / LR, X = 16 / sizeof(TS);
   constexpr int VP = kTile + 4 / sizeof(TS);  // pitch of a dim's row of values
+  constexpr size_t kTrig = ROT == kNoRotation ? 16 : 2 * RP * (HD / 2) * sizeof(float), kValues = HD * VP * sizeof(TS);
   __shared__ TilePlan t;
-  __shared__ TS vt[HD * VP];
-  __shared__ float cs[ROT ? kTile * 64 : 1], sn[ROT ? kTile * 64 : 1];
+  __shared__ __align__(16) char lds[kTrig > kValues ? kTrig : kValues];
   const int tid = threadIdx.x, row0 = blockIdx.x * kTile;
-  const int h0 = blockIdx.y * p.heads_per_wg, h1 = min(h0 + p.heads_per_wg, p.st.n_kv);
   const int64_t bs = (int64_t)1 << p.st.bs_log2;
+  const int c = tid % LR, d0 = 16 * c;
   if (tid < kTile) plan_tile<X>(p, row0, t);
   __syncthreads();
-  if constexpr (ROT) {
-    const int half = rot.rotary_dim >> 1;
-    for (int e = tid; e < kTile * half; e += 256) {
-      const int r = e / half, i = e % half;
-      if (t.dest[r] < 0) continue;
-      float c, s;
-      cos_sin_turns((double)p.positions[row0 + r] * rot.turns[i], c, s);
-      cs[r * 64 + i] = c * rot.scale;
-      sn[r * 64 + i] = s * rot.scale;
-    }
-    __syncthreads();
-  }
-  for (int h = h0; h < h1; ++h) {
-    for (int r = tid / LR; r < kTile; r += RP) {
-      const int c = tid % LR, d0 = 16 * c;
+  if ((int)blockIdx.y >= p.st.n_kv) {  // keys
+    float* cs = (float*)lds;
+    float* sn = cs + RP * (HD / 2);
+    const int h0 = ((int)blockIdx.y - p.st.n_kv) * p.heads_per_wg, h1 = min(h0 + p.heads_per_wg, p.st.n_kv);
+    for (int r0 = 0; r0 < kTile; r0 += RP) {
+      if constexpr (ROT != kNoRotation) {
+        if (r0) __syncthreads();
+        const int half = rot.rotary_dim >> 1;
+        for (int e = tid; e < RP * half; e += 256) {
+          const int r = e / half, i = e - r * half;
+          if (t.dest[r0 + r] < 0) continue;
+          float co, si;
+          cos_sin_turns((double)p.positions[row0 + r0 + r] * rot.turns[i], co, si);
+          cs[r * (HD / 2) + i] = co * rot.scale;
+          sn[r * (HD / 2) + i] = si * rot.scale;
+        }
+        __syncthreads();
+      }
+      const int rr = tid / LR, r = r0 + rr;
       const int64_t dest = t.dest[r];
       if (dest < 0) continue;  // (the LR lanes of a row alike)
       const int64_t blk = dest >> p.st.bs_log2, slot = dest & (bs - 1);
-      float x[16];
-      const TI* kr = (const TI*)p.k.data + (int64_t)t.src[r] * p.k.row + h * p.k.head;
-      load16(kr + d0, p.k_vec, x);
-      if constexpr (ROT) {
+      const TI* kr = (const TI*)p.k.data + (int64_t)t.src[r] * p.k.row;
+      for (int h = h0; h < h1; ++h) {
+        float x[16];
+        const TI* kh = kr + h * p.k.head;
+        load16(kh + d0, p.k_vec, x);
+        if constexpr (ROT == kHalf16) {
+          const int half = rot.rotary_dim >> 1;
+          if (d0 < rot.rotary_dim) {
+            const bool first = d0 < half;
+            const float* co = cs + rr * (HD / 2) + (first ? d0 : d0 - half);
+            const float* si = sn + rr * (HD / 2) + (first ? d0 : d0 - half);
+            float y[16];
+            load16(kh + (first ? d0 + half : d0 - half), p.k_vec, y);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int d = d0 + i;
-          if (d >= rot.rotary_dim) continue;
-          const PairOf o = pair_of(d, rot.rotary_dim, rot.layout);
-          const float y = to_f32(kr[o.other]), co = cs[r * 64 + o.pair], si = sn[r * 64 + o.pair];
-          x[i] = o.first ? x[i] * co - y * si : x[i] * co + y * si;
+            for (int i = 0; i < 16; ++i) x[i] = first ? x[i] * co[i] - y[i] * si[i] : x[i] * co[i] + y[i] * si[i];
+          }
+        } else if constexpr (ROT == kAnyRotation) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int d = d0 + i;
+            if (d >= rot.rotary_dim) continue;
+            const PairOf o = pair_of(d, rot.rotary_dim, rot.layout);
+            const float y = to_f32(kh[o.other]), co = cs[rr * (HD / 2) + o.pair], si = sn[rr * (HD / 2) + o.pair];
+            x[i] = o.first ? x[i] * co - y * si : x[i] * co + y * si;
+          }
+        }
+        Stored<TS> w;
+        int biased = 0;
+        pack<TS, LR>(x, w, biased);
+        TS* kb = (TS*)p.st.k + blk * p.st.k_sb + h * p.st.k_sh;
+        if constexpr (sizeof(TS) == 1) {
+          *reinterpret_cast<u32x4*>(kb + ((int64_t)c * bs + slot) * X) = w.w;
+          if (c == 0) p.st.k_exp[blk * p.st.e_sb + h * p.st.e_sh + slot] = (uint8_t)biased;
+        } else {
+#pragma unroll
+          for (int q = 0; q < 16 / X; ++q) {
+            u32x4 piece;
+            __builtin_memcpy(&piece, &w.v[q * X], 16);
+            *reinterpret_cast<u32x4*>(kb + ((int64_t)(c * (16 / X) + q) * bs + slot) * X) = piece;
+          }
         }
       }
-      Stored<TS> w;
-      int biased = 0;
-      pack<TS, LR>(x, w, biased);
-      TS* kb = (TS*)p.st.k + blk * p.st.k_sb + h * p.st.k_sh;
-      if constexpr (sizeof(TS) == 1) {
-        *reinterpret_cast<u32x4*>(kb + ((int64_t)c * bs + slot) * X) = w.w;
-        if (c == 0) p.st.k_exp[blk * p.st.e_sb + h * p.st.e_sh + slot] = (uint8_t)biased;
-      } else {
-#pragma unroll
-        for (int q = 0; q < 16 / X; ++q) {
-          u32x4 piece;
-          __builtin_memcpy(&piece, &w.v[q * X], 16);
-          *reinterpret_cast<u32x4*>(kb + ((int64_t)(c * (16 / X) + q) * bs + slot) * X) = piece;
-        }
-      }
-      load16((const TI*)p.v.data + (int64_t)t.src[r] * p.v.row + h * p.v.head + d0, p.v_vec, x);
-      pack<TS, LR>(x, w, biased);
-      if constexpr (sizeof(TS) == 1) {
-        if (c == 0) p.st.v_exp[blk * p.st.e_sb + h * p.st.e_sh + slot] = (uint8_t)biased;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) vt[(d0 + i) * VP + r].bits = (uint8_t)(w.w[i / 4] >> (8 * (i % 4)));
-      } else {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) vt[(d0 + i) * VP + r] = w.v[i];
-      }
     }
-    __syncthreads();
-    const int nl = t.n_lead, ns = t.n_single;
-    for (int e = tid; e < nl * HD; e += 256) {
-      const int r = t.lead[e % nl], d = e / nl;
-      const int64_t dest = t.dest[r], blk = dest >> p.st.bs_log2, slot = dest & (bs - 1);
-      TS piece[X];
+    return;
+  }
+  // values
+  TS* vt = (TS*)lds;
+  const int h = blockIdx.y;
+  for (int r = tid / LR; r < kTile; r += RP) {
+    const int64_t dest = t.dest[r];
+    if (dest < 0) continue;
+    const int64_t blk = dest >> p.st.bs_log2, slot = dest & (bs - 1);
+    float x[16];
+    Stored<TS> w;
+    int biased = 0;
+    load16((const TI*)p.v.data + (int64_t)t.src[r] * p.v.row + h * p.v.head + d0, p.v_vec, x);
+    pack<TS, LR>(x, w, biased);
+    if constexpr (sizeof(TS) == 1) {
+      if (c == 0) p.st.v_exp[blk * p.st.e_sb + h * p.st.e_sh + slot] = (uint8_t)biased;
 #pragma unroll
-      for (int i = 0; i < X; ++i) piece[i] = vt[d * VP + r + i];
-      u32x4 w;
-      __builtin_memcpy(&w, piece, 16);
-      *reinterpret_cast<u32x4*>((TS*)p.st.v + blk * p.st.v_sb + h * p.st.v_sh + d * bs + slot) = w;
+      for (int i = 0; i < 16; ++i) vt[(d0 + i) * VP + r].bits = (uint8_t)(w.w[i / 4] >> (8 * (i % 4)));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) vt[(d0 + i) * VP + r] = w.v[i];
     }
-    for (int e = tid; e < ns * HD; e += 256) {
-      const int r = t.single[e / HD], d = e % HD;
-      const int64_t dest = t.dest[r], blk = dest >> p.st.bs_log2, slot = dest & (bs - 1);
-      ((TS*)p.st.v)[blk * p.st.v_sb + h * p.st.v_sh + d * bs + slot] = vt[d * VP + r];
-    }
-    __syncthreads();
+  }
+  __syncthreads();
+  const int nl = t.n_lead, ns = t.n_single;
+  for (int e = tid; e < nl * HD; e += 256) {
+    const int d = e / nl, r = t.lead[e - d * nl];
+    const int64_t dest = t.dest[r], blk = dest >> p.st.bs_log2, slot = dest & (bs - 1);
+    TS piece[X];
+#pragma unroll
+    for (int i = 0; i < X; ++i) piece[i] = vt[d * VP + r + i];
+    u32x4 w;
+    __builtin_memcpy(&w, piece, 16);
+    *reinterpret_cast<u32x4*>((TS*)p.st.v + blk * p.st.v_sb + h * p.st.v_sh + d * bs + slot) = w;
+  }
+  for (int e = tid; e < ns * HD; e += 256) {
+    const int r = t.single[e / HD], d = e % HD;
+    const int64_t dest = t.dest[r], blk = dest >> p.st.bs_log2, slot = dest & (bs - 1);
+    ((TS*)p.st.v)[blk * p.st.v_sb + h * p.st.v_sh + d * bs + slot] = vt[d * VP + r];
   }
 }
 
 // ---------------------------------------------------------------- read
-// The same tiles the other way: values through LDS, by groups where the tokens make them.
+// The same tiles the other way, a workgroup per KV head for the keys and one for the values: values
+// through LDS, by groups where the tokens make them.
 template <typename TS>
 __device__ __forceinline__ float value_of(TS x) {
   if constexpr (sizeof(TS) == 1) return __builtin_amdgcn_cvt_f32_fp8((int)x.bits, 0);
@@ -345,76 +416,71 @@ __global__ __launch_bounds__(256) void cache_read(const CacheParams p) {
   __shared__ TilePlan t;
   __shared__ TS vt[HD * VP];
   const int tid = threadIdx.x, row0 = blockIdx.x * kTile;
-  const int h0 = blockIdx.y * p.heads_per_wg, h1 = min(h0 + p.heads_per_wg, p.st.n_kv);
   const int64_t bs = (int64_t)1 << p.st.bs_log2;
+  const int c = tid % LR, d0 = 16 * c;
+  const bool keys = p.k.data && (int)blockIdx.y < p.st.n_kv;
+  const int h = blockIdx.y % p.st.n_kv;
   if (tid < kTile) plan_tile<X>(p, row0, t);
   __syncthreads();
-  const int nl = t.n_lead, ns = t.n_single;
-  for (int h = h0; h < h1; ++h) {
-    if (p.v.data) {
-      for (int e = tid; e < nl * HD; e += 256) {
-        const int r = t.lead[e % nl], d = e / nl;
-        const int64_t dest = t.dest[r], blk = dest >> p.st.bs_log2, slot = dest & (bs - 1);
-        const u32x4 w = ld16v((const TS*)p.st.v + blk * p.st.v_sb + h * p.st.v_sh + d * bs + slot);
-        TS piece[X];
-        __builtin_memcpy(piece, &w, 16);
+  if (!keys) {
+    const int nl = t.n_lead, ns = t.n_single;
+    for (int e = tid; e < nl * HD; e += 256) {
+      const int d = e / nl, r = t.lead[e - d * nl];
+      const int64_t dest = t.dest[r], blk = dest >> p.st.bs_log2, slot = dest & (bs - 1);
+      const u32x4 w = ld16v((const TS*)p.st.v + blk * p.st.v_sb + h * p.st.v_sh + d * bs + slot);
+      TS piece[X];
+      __builtin_memcpy(piece, &w, 16);
 #pragma unroll
-        for (int i = 0; i < X; ++i) vt[d * VP + r + i] = piece[i];
-      }
-      for (int e = tid; e < ns * HD; e += 256) {
-        const int r = t.single[e / HD], d = e % HD;
-        const int64_t dest = t.dest[r], blk = dest >> p.st.bs_log2, slot = dest & (bs - 1);
-        vt[d * VP + r] = ((const TS*)p.st.v)[blk * p.st.v_sb + h * p.st.v_sh + d * bs + slot];
-      }
+      for (int i = 0; i < X; ++i) vt[d * VP + r + i] = piece[i];
     }
-    __syncthreads();
-    for (int r = tid / LR; r < kTile; r += RP) {
-      const int c = tid % LR, d0 = 16 * c;
-      const int64_t dest = t.dest[r];
-      if (dest < 0) continue;
-      const int64_t blk = dest >> p.st.bs_log2, slot = dest & (bs - 1);
-      const int64_t row = row0 + r;
-      float x[16];
-      if (p.k.data) {
-        const TS* kb = (const TS*)p.st.k + blk * p.st.k_sb + h * p.st.k_sh;
-        float f = 1.f;
-        if constexpr (sizeof(TS) == 1) f = power_of(p.st.k_exp[blk * p.st.e_sb + h * p.st.e_sh + slot]);
-#pragma unroll
-        for (int q = 0; q < 16 / X; ++q) {
-          const u32x4 w = ld16v(kb + ((int64_t)(c * (16 / X) + q) * bs + slot) * X);
-          TS piece[X];
-          __builtin_memcpy(piece, &w, 16);
-#pragma unroll
-          for (int i = 0; i < X; ++i) x[q * X + i] = value_of(piece[i]) * f;
-        }
-        store16((TI*)p.k.data + row * p.k.row + h * p.k.head + d0, p.k_vec, x);
-      }
-      if (p.v.data) {
-        float f = 1.f;
-        if constexpr (sizeof(TS) == 1) f = power_of(p.st.v_exp[blk * p.st.e_sb + h * p.st.e_sh + slot]);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = value_of(vt[(d0 + i) * VP + r]) * f;
-        store16((TI*)p.v.data + row * p.v.row + h * p.v.head + d0, p.v_vec, x);
-      }
+    for (int e = tid; e < ns * HD; e += 256) {
+      const int r = t.single[e / HD], d = e % HD;
+      const int64_t dest = t.dest[r], blk = dest >> p.st.bs_log2, slot = dest & (bs - 1);
+      vt[d * VP + r] = ((const TS*)p.st.v)[blk * p.st.v_sb + h * p.st.v_sh + d * bs + slot];
     }
     __syncthreads();
   }
+  for (int r = tid / LR; r < kTile; r += RP) {
+    const int64_t dest = t.dest[r];
+    if (dest < 0) continue;
+    const int64_t blk = dest >> p.st.bs_log2, slot = dest & (bs - 1), row = row0 + r;
+    float x[16], f = 1.f;
+    if constexpr (sizeof(TS) == 1) f = power_of((keys ? p.st.k_exp : p.st.v_exp)[blk * p.st.e_sb + h * p.st.e_sh + slot]);
+    if (keys) {
+      const TS* kb = (const TS*)p.st.k + blk * p.st.k_sb + h * p.st.k_sh;
+#pragma unroll
+      for (int q = 0; q < 16 / X; ++q) {
+        const u32x4 w = ld16v(kb + ((int64_t)(c * (16 / X) + q) * bs + slot) * X);
+        TS piece[X];
+        __builtin_memcpy(piece, &w, 16);
+#pragma unroll
+        for (int i = 0; i < X; ++i) x[q * X + i] = value_of(piece[i]) * f;
+      }
+      store16((TI*)p.k.data + row * p.k.row + h * p.k.head + d0, p.k_vec, x);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = value_of(vt[(d0 + i) * VP + r]) * f;
+      store16((TI*)p.v.data + row * p.v.row + h * p.v.head + d0, p.v_vec, x);
+    }
+  }
+}
+
+template <typename TS, typename TI, int HD>
+hipError_t write_hd(const CacheParams& p, dim3 grid, hipStream_t s) {
+  const sp_rotary none{};
+  CacheParams d = p;
+  d.rot = nullptr;
+  const dim3 block(256);
+  if (!p.rot) hipLaunchKernelGGL((cache_write<TS, TI, HD, kNoRotation>), grid, block, 0, s, d, none);
+  else if (p.rot->layout == SP_ROTARY_HALF && p.rot->rotary_dim % 32 == 0)
+    hipLaunchKernelGGL((cache_write<TS, TI, HD, kHalf16>), grid, block, 0, s, d, *p.rot);
+  else hipLaunchKernelGGL((cache_write<TS, TI, HD, kAnyRotation>), grid, block, 0, s, d, *p.rot);
+  return hipGetLastError();
 }
 
 template <typename TS, typename TI>
 hipError_t write_typed(const CacheParams& p, int hd, dim3 grid, hipStream_t s) {
-  const sp_rotary none{};
-  const sp_rotary& r = p.rot ? *p.rot : none;
-  CacheParams d = p;
-  d.rot = nullptr;
-  if (hd == 128) {
-    if (p.rot) hipLaunchKernelGGL((cache_write<TS, TI, 128, true>), grid, dim3(256), 0, s, d, r);
-    else hipLaunchKernelGGL((cache_write<TS, TI, 128, false>), grid, dim3(256), 0, s, d, r);
-  } else {
-    if (p.rot) hipLaunchKernelGGL((cache_write<TS, TI, 64, true>), grid, dim3(256), 0, s, d, r);
-    else hipLaunchKernelGGL((cache_write<TS, TI, 64, false>), grid, dim3(256), 0, s, d, r);
-  }
-  return hipGetLastError();
+  return hd == 128 ? write_hd<TS, TI, 128>(p, grid, s) : write_hd<TS, TI, 64>(p, grid, s);
 }
 
 template <typename TS, typename TI>
@@ -424,31 +490,41 @@ hipError_t read_typed(const CacheParams& p, int hd, dim3 grid, hipStream_t s) {
   return hipGetLastError();
 }
 
-// KV heads per workgroup: as many as leave two workgroups per compute unit (the places and
-// the angles of a tile are found once for all of them).
+// KV heads of a workgroup of keys: one, or with a rotation as many as leave four workgroups per
+// compute unit (their angles are found once).
 int heads_per_wg(const CacheParams& p, int n_cus) {
+  if (!p.rot) return 1;
   const int64_t tiles = (p.n_rows + kTile - 1) / kTile;
   int hpw = p.st.n_kv;
-  while (hpw > 1 && tiles * ((p.st.n_kv + hpw - 1) / hpw) < 2 * (int64_t)n_cus) hpw = (hpw + 1) / 2;
+  while (hpw > 1 && tiles * ((p.st.n_kv + hpw - 1) / hpw) < 4 * (int64_t)n_cus) hpw = (hpw + 1) / 2;
   return hpw;
+}
+
+template <typename T, int R>
+hipError_t rotary_typed(const RotaryParams& p, hipStream_t s) {
+  constexpr int V = 16 / sizeof(T);
+  const dim3 grid((p.n_rows + R - 1) / R), block(256);
+  if (p.vec && p.rot.layout == SP_ROTARY_INTERLEAVED) hipLaunchKernelGGL((rotary_rows<T, kInterleaved, R>), grid, block, 0, s, p);
+  else if (p.vec && p.rot.rotary_dim % (2 * V) == 0) hipLaunchKernelGGL((rotary_rows<T, kHalf, R>), grid, block, 0, s, p);
+  else hipLaunchKernelGGL((rotary_rows<T, kScalar, R>), grid, block, 0, s, p);
+  return hipGetLastError();
 }
 
 }  // namespace
 
+// Four rows a workgroup where that leaves four workgroups per compute unit, else one.
 hipError_t launch_rotary(const RotaryParams& p, int bf16_rows, int n_cus, hipStream_t s) {
-  (void)n_cus;
   if (p.n_rows <= 0) return hipSuccess;
-  const dim3 grid(p.n_rows), block(256);
-  if (bf16_rows) hipLaunchKernelGGL((rotary_rows<bf16>), grid, block, 0, s, p);
-  else hipLaunchKernelGGL((rotary_rows<float>), grid, block, 0, s, p);
-  return hipGetLastError();
+  if (p.n_rows >= 4 * kRotaryRows * n_cus)
+    return bf16_rows ? rotary_typed<bf16, kRotaryRows>(p, s) : rotary_typed<float, kRotaryRows>(p, s);
+  return bf16_rows ? rotary_typed<bf16, 1>(p, s) : rotary_typed<float, 1>(p, s);
 }
 
 hipError_t launch_cache_write(const CacheParams& p0, int storage, int bf16_rows, int hd, int n_cus, hipStream_t s) {
   if (p0.n_rows <= 0) return hipSuccess;
   CacheParams p = p0;
   p.heads_per_wg = heads_per_wg(p, n_cus);
-  const dim3 grid((p.n_rows + kTile - 1) / kTile, (p.st.n_kv + p.heads_per_wg - 1) / p.heads_per_wg);
+  const dim3 grid((p.n_rows + kTile - 1) / kTile, p.st.n_kv + (p.st.n_kv + p.heads_per_wg - 1) / p.heads_per_wg);
   switch (storage) {
     case SP_F32: return bf16_rows ? write_typed<float, bf16>(p, hd, grid, s) : write_typed<float, float>(p, hd, grid, s);
     case SP_BF16: return bf16_rows ? write_typed<bf16, bf16>(p, hd, grid, s) : write_typed<bf16, float>(p, hd, grid, s);
@@ -457,11 +533,9 @@ hipError_t launch_cache_write(const CacheParams& p0, int storage, int bf16_rows,
   return hipErrorInvalidValue;
 }
 
-hipError_t launch_cache_read(const CacheParams& p0, int storage, int bf16_rows, int hd, int n_cus, hipStream_t s) {
-  if (p0.n_rows <= 0) return hipSuccess;
-  CacheParams p = p0;
-  p.heads_per_wg = heads_per_wg(p, n_cus);
-  const dim3 grid((p.n_rows + kTile - 1) / kTile, (p.st.n_kv + p.heads_per_wg - 1) / p.heads_per_wg);
+hipError_t launch_cache_read(const CacheParams& p, int storage, int bf16_rows, int hd, hipStream_t s) {
+  if (p.n_rows <= 0) return hipSuccess;
+  const dim3 grid((p.n_rows + kTile - 1) / kTile, p.st.n_kv * ((p.k.data != nullptr) + (p.v.data != nullptr)));
   switch (storage) {
     case SP_F32: return bf16_rows ? read_typed<float, bf16>(p, hd, grid, s) : read_typed<float, float>(p, hd, grid, s);
     case SP_BF16: return bf16_rows ? read_typed<bf16, bf16>(p, hd, grid, s) : read_typed<bf16, float>(p, hd, grid, s);

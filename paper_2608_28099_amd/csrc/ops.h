@@ -48,7 +48,7 @@ struct CacheParams {
 };
 // storage: SP_F32, SP_BF16 or SP_E4M3; bf16: type of the rows.
 hipError_t launch_cache_write(const CacheParams& p, int storage, int bf16, int hd, int n_cus, hipStream_t s);
-hipError_t launch_cache_read(const CacheParams& p, int storage, int bf16, int hd, int n_cus, hipStream_t s);
+hipError_t launch_cache_read(const CacheParams& p, int storage, int bf16, int hd, hipStream_t s);
 
 // ---------------------------------------------------------------- tree attention
 struct TreeParams {

@@ -342,7 +342,7 @@ SP_API int sp_probe_cache_read(const sp_kv_store* store, const int32_t* block_ta
   int cus = 0;
   if ((st = current_device(&cus)) != SP_OK) return st;
   p.n_src = n_rows;
-  return launch_cache_read(p, store->dtype, dtype == SP_BF16, store->head_dim, cus, (hipStream_t)stream) == hipSuccess
+  return launch_cache_read(p, store->dtype, dtype == SP_BF16, store->head_dim, (hipStream_t)stream) == hipSuccess
              ? SP_OK : SP_ERR_HIP;
 }
 
