@@ -10,28 +10,53 @@ namespace {
 struct e4m3 { uint8_t bits; };  // storage tag
 
 // ---------------------------------------------------------------- sixteen values of a head
-// The lane's 16 consecutive values in fp32; `vec`: 16-byte aligned.
+// A lane's 16 consecutive values as they lie in memory; `vec`: 16-byte aligned.
 template <typename T>
-__device__ __forceinline__ void load16(const T* p, bool vec, float (&x)[16]) {
+struct Raw16 {
+  u32x4 w[sizeof(T)];
+};
+
+template <typename T>
+__device__ __forceinline__ Raw16<T> load_raw(const T* p, bool vec) {
+  Raw16<T> x;
   if (vec) {
-    if constexpr (sizeof(T) == 2) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const bf16x8 w = __builtin_bit_cast(bf16x8, ld16v(p + 8 * h));
+    for (int i = 0; i < (int)sizeof(T); ++i) x.w[i] = ld16v((const char*)p + 16 * i);
+  } else {
+    T v[16];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[8 * h + i] = (float)w[i];
-      }
-    } else {
+    for (int i = 0; i < 16; ++i) v[i] = p[i];
+    __builtin_memcpy(&x, v, sizeof(x));
+  }
+  return x;
+}
+
+// The same of two runs of 8.
+template <typename T>
+__device__ __forceinline__ Raw16<T> load_raw(const T* p, const T* q, bool vec) {
+  constexpr int N = sizeof(T) / 2;
+  Raw16<T> x;
+  if (vec) {
 #pragma unroll
-      for (int h = 0; h < 4; ++h) {
-        const f32x4 w = *reinterpret_cast<const f32x4*>(p + 4 * h);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[4 * h + i] = w[i];
-      }
+    for (int i = 0; i < N; ++i) {
+      x.w[i] = ld16v((const char*)p + 16 * i);
+      x.w[N + i] = ld16v((const char*)q + 16 * i);
     }
   } else {
+    T v[16];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = to_f32(p[i]);
+    for (int i = 0; i < 16; ++i) v[i] = i < 8 ? p[i] : q[i - 8];
+    __builtin_memcpy(&x, v, sizeof(x));
+  }
+  return x;
+}
+
+template <typename T>
+__device__ __forceinline__ void unpack(const Raw16<T>& r, float (&x)[16]) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const uint32_t w = r.w[i * sizeof(T) / 16][i * sizeof(T) / 4 % 4];
+    x[i] = __builtin_bit_cast(float, sizeof(T) == 4 ? w : i & 1 ? w & 0xffff0000u : w << 16);
   }
 }
 
@@ -279,13 +304,16 @@ __device__ __forceinline__ void plan_tile(const CacheParams& p, int row0, TilePl
   }
 }
 
-enum KeyRotation { kNoRotation, kAnyRotation, kHalf16 };  // kHalf16: half layout, rotary_dim / 2 a multiple of 16
+// How keys are rotated.  kHalf8: half layout, rotary_dim / 2 a multiple of 8: a lane takes two runs of 8
+// values that pair with each other; kPairs: interleaved, pairs within the lane's 16; kAny: any half layout.
+enum KeyRotation { kNoRotation, kHalf8, kPairs, kAny };
 
 template <typename TS, typename TI, int HD, int ROT>
 __global__ __launch_bounds__(256) void cache_write(const CacheParams p, const sp_rotary rot) {
   constexpr int LR = HD / 16, RP = 256 / LR, X = 16 / sizeof(TS);
   constexpr int VP = kTile + 4 / sizeof(TS);  // pitch of a dim's row of values
-  constexpr size_t kTrig = ROT == kNoRotation ? 16 : 2 * RP * (HD / 2) * sizeof(float), kValues = HD * VP * sizeof(TS);
+  constexpr int TP = HD / 2 + 4;              // pitch of a row's cosines (rows on different banks)
+  constexpr size_t kTrig = ROT == kNoRotation ? 16 : 2 * RP * TP * sizeof(float), kValues = HD * VP * sizeof(TS);
   __shared__ TilePlan t;
   __shared__ __align__(16) char lds[kTrig > kValues ? kTrig : kValues];
   const int tid = threadIdx.x, row0 = blockIdx.x * kTile;
@@ -295,67 +323,87 @@ __global__ __launch_bounds__(256) void cache_write(const CacheParams p, const sp
   __syncthreads();
   if ((int)blockIdx.y >= p.st.n_kv) {  // keys
     float* cs = (float*)lds;
-    float* sn = cs + RP * (HD / 2);
+    float* sn = cs + RP * TP;
     const int h0 = ((int)blockIdx.y - p.st.n_kv) * p.heads_per_wg, h1 = min(h0 + p.heads_per_wg, p.st.n_kv);
+    const int rd = rot.rotary_dim, half = rd >> 1;
+    // first values of the lane's two runs of 8 (which lie side by side but for the pairs of kHalf8)
+    const bool turns = ROT == kHalf8 && d0 < rd;
+    const int da = turns ? 8 * c : d0, db = turns ? half + 8 * c : d0 + 8;
     for (int r0 = 0; r0 < kTile; r0 += RP) {
+      const int rr = tid / LR, r = r0 + rr;
+      const int64_t dest = t.dest[r];
+      const int64_t blk = dest >> p.st.bs_log2, slot = dest & (bs - 1);
+      const TI* kr = (const TI*)p.k.data + (int64_t)t.src[r] * p.k.row;
+      // the next head's values are under way while this one's are rotated, packed and stored
+      Raw16<TI> x;
+      if (dest >= 0) x = load_raw(kr + h0 * p.k.head + da, kr + h0 * p.k.head + db, p.k_vec);
       if constexpr (ROT != kNoRotation) {
         if (r0) __syncthreads();
-        const int half = rot.rotary_dim >> 1;
         for (int e = tid; e < RP * half; e += 256) {
-          const int r = e / half, i = e - r * half;
-          if (t.dest[r0 + r] < 0) continue;
+          const int q = e / half, i = e - q * half;
+          if (t.dest[r0 + q] < 0) continue;
           float co, si;
-          cos_sin_turns((double)p.positions[row0 + r0 + r] * rot.turns[i], co, si);
-          cs[r * (HD / 2) + i] = co * rot.scale;
-          sn[r * (HD / 2) + i] = si * rot.scale;
+          cos_sin_turns((double)p.positions[row0 + r0 + q] * rot.turns[i], co, si);
+          cs[q * TP + i] = co * rot.scale;
+          sn[q * TP + i] = si * rot.scale;
         }
         __syncthreads();
       }
-      const int rr = tid / LR, r = r0 + rr;
-      const int64_t dest = t.dest[r];
       if (dest < 0) continue;  // (the LR lanes of a row alike)
-      const int64_t blk = dest >> p.st.bs_log2, slot = dest & (bs - 1);
-      const TI* kr = (const TI*)p.k.data + (int64_t)t.src[r] * p.k.row;
+      const float* co = cs + rr * TP;
+      const float* si = sn + rr * TP;
       for (int h = h0; h < h1; ++h) {
-        float x[16];
-        const TI* kh = kr + h * p.k.head;
-        load16(kh + d0, p.k_vec, x);
-        if constexpr (ROT == kHalf16) {
-          const int half = rot.rotary_dim >> 1;
-          if (d0 < rot.rotary_dim) {
-            const bool first = d0 < half;
-            const float* co = cs + rr * (HD / 2) + (first ? d0 : d0 - half);
-            const float* si = sn + rr * (HD / 2) + (first ? d0 : d0 - half);
-            float y[16];
-            load16(kh + (first ? d0 + half : d0 - half), p.k_vec, y);
+        Raw16<TI> x1;
+        if (h + 1 < h1) x1 = load_raw(kr + (h + 1) * p.k.head + da, kr + (h + 1) * p.k.head + db, p.k_vec);
+        float k[16];
+        unpack(x, k);
+        if constexpr (ROT == kHalf8) {
+          if (turns)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] = first ? x[i] * co[i] - y[i] * si[i] : x[i] * co[i] + y[i] * si[i];
+            for (int i = 0; i < 8; ++i) {
+              const float a = k[i], b = k[8 + i], cc = co[da + i], ss = si[da + i];
+              k[i] = a * cc - b * ss;
+              k[8 + i] = b * cc + a * ss;
+            }
+        } else if constexpr (ROT == kPairs) {
+#pragma unroll
+          for (int i = 0; i < 16; i += 2) {
+            if (d0 + i >= rd) continue;
+            const float a = k[i], b = k[i + 1], cc = co[d0 / 2 + i / 2], ss = si[d0 / 2 + i / 2];
+            k[i] = a * cc - b * ss;
+            k[i + 1] = b * cc + a * ss;
           }
-        } else if constexpr (ROT == kAnyRotation) {
+        } else if constexpr (ROT == kAny) {
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            const int d = d0 + i;
-            if (d >= rot.rotary_dim) continue;
-            const PairOf o = pair_of(d, rot.rotary_dim, rot.layout);
-            const float y = to_f32(kh[o.other]), co = cs[rr * (HD / 2) + o.pair], si = sn[rr * (HD / 2) + o.pair];
-            x[i] = o.first ? x[i] * co - y * si : x[i] * co + y * si;
+            if (d0 + i >= rd) continue;
+            const PairOf o = pair_of(d0 + i, rd, rot.layout);
+            const float z = to_f32(kr[h * p.k.head + o.other]);
+            k[i] = o.first ? k[i] * co[o.pair] - z * si[o.pair] : k[i] * co[o.pair] + z * si[o.pair];
           }
         }
         Stored<TS> w;
         int biased = 0;
-        pack<TS, LR>(x, w, biased);
+        pack<TS, LR>(k, w, biased);
         TS* kb = (TS*)p.st.k + blk * p.st.k_sb + h * p.st.k_sh;
         if constexpr (sizeof(TS) == 1) {
-          *reinterpret_cast<u32x4*>(kb + ((int64_t)c * bs + slot) * X) = w.w;
+          if constexpr (ROT == kHalf8) {
+            *reinterpret_cast<u32x2*>(kb + ((int64_t)(da / X) * bs + slot) * X + da % X) = u32x2{w.w[0], w.w[1]};
+            *reinterpret_cast<u32x2*>(kb + ((int64_t)(db / X) * bs + slot) * X + db % X) = u32x2{w.w[2], w.w[3]};
+          } else {
+            *reinterpret_cast<u32x4*>(kb + ((int64_t)c * bs + slot) * X) = w.w;
+          }
           if (c == 0) p.st.k_exp[blk * p.st.e_sb + h * p.st.e_sh + slot] = (uint8_t)biased;
         } else {
 #pragma unroll
           for (int q = 0; q < 16 / X; ++q) {
+            const int d = q < 8 / X ? da + q * X : db + (q - 8 / X) * X;
             u32x4 piece;
             __builtin_memcpy(&piece, &w.v[q * X], 16);
-            *reinterpret_cast<u32x4*>(kb + ((int64_t)(c * (16 / X) + q) * bs + slot) * X) = piece;
+            *reinterpret_cast<u32x4*>(kb + ((int64_t)(d / X) * bs + slot) * X) = piece;
           }
         }
+        x = x1;
       }
     }
     return;
@@ -370,7 +418,7 @@ __global__ __launch_bounds__(256) void cache_write(const CacheParams p, const sp
     float x[16];
     Stored<TS> w;
     int biased = 0;
-    load16((const TI*)p.v.data + (int64_t)t.src[r] * p.v.row + h * p.v.head + d0, p.v_vec, x);
+    unpack(load_raw((const TI*)p.v.data + (int64_t)t.src[r] * p.v.row + h * p.v.head + d0, p.v_vec), x);
     pack<TS, LR>(x, w, biased);
     if constexpr (sizeof(TS) == 1) {
       if (c == 0) p.st.v_exp[blk * p.st.e_sb + h * p.st.e_sh + slot] = (uint8_t)biased;
@@ -472,9 +520,11 @@ hipError_t write_hd(const CacheParams& p, dim3 grid, hipStream_t s) {
   d.rot = nullptr;
   const dim3 block(256);
   if (!p.rot) hipLaunchKernelGGL((cache_write<TS, TI, HD, kNoRotation>), grid, block, 0, s, d, none);
-  else if (p.rot->layout == SP_ROTARY_HALF && p.rot->rotary_dim % 32 == 0)
-    hipLaunchKernelGGL((cache_write<TS, TI, HD, kHalf16>), grid, block, 0, s, d, *p.rot);
-  else hipLaunchKernelGGL((cache_write<TS, TI, HD, kAnyRotation>), grid, block, 0, s, d, *p.rot);
+  else if (p.rot->layout == SP_ROTARY_HALF && p.rot->rotary_dim % 16 == 0)
+    hipLaunchKernelGGL((cache_write<TS, TI, HD, kHalf8>), grid, block, 0, s, d, *p.rot);
+  else if (p.rot->layout == SP_ROTARY_INTERLEAVED)
+    hipLaunchKernelGGL((cache_write<TS, TI, HD, kPairs>), grid, block, 0, s, d, *p.rot);
+  else hipLaunchKernelGGL((cache_write<TS, TI, HD, kAny>), grid, block, 0, s, d, *p.rot);
   return hipGetLastError();
 }
 
