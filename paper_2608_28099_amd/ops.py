@@ -36,38 +36,28 @@ def _need(ok, what):
         raise ValueError(what)
 
 
-class _Call:
-    """The device guard and stream of one call.  (The checks of a call spell out what is wrong
-    only where they fail: a call's host time is of the order of its kernel's.)"""
+# Every call runs with its tensors' device current (else it calls itself under a guard) and on
+# the raw handle of the given or current stream.  The checks of a call spell out what is wrong
+# only where they fail: a call's host time is of the order of its kernel's.
+_current_device = torch.cuda.current_device
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+    (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
-    __slots__ = ("device", "given", "guard", "stream")
 
-    def __init__(self, device, stream):
-        if device.type != "cuda":
-            raise ValueError("tensors must be on the GPU")
-        self.device, self.given, self.guard = device, stream, None
-        index = device.index
-        if index is not None and index != torch.cuda.current_device():
-            self.guard = torch.cuda.device(device)
+def _elsewhere(device):
+    """Whether `device` is not the current one."""
+    if device.type != "cuda":
+        raise ValueError("tensors must be on the GPU")
+    return device.index is not None and device.index != _current_device()
 
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        self.stream = torch.cuda.current_stream(self.device).cuda_stream if self.given is None else self.given
-        return self
 
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
-        return False
-
-    def hold(self, *tensors):
-        """Memory that this call made lives until the given stream is past it."""
-        if self.given is not None:
-            s = torch.cuda.ExternalStream(self.given, device=self.device)
-            for t in tensors:
-                if t is not None:
-                    t.record_stream(s)
+def _hold(stream, device, *tensors):
+    """Memory that a call made lives until the given stream is past it."""
+    if stream is not None:
+        s = torch.cuda.ExternalStream(stream, device=device)
+        for t in tensors:
+            if t is not None:
+                t.record_stream(s)
 
 
 def _check(status, what):
@@ -127,24 +117,27 @@ def rotary(rot, positions, q, k=None, out=None, k_out=None, transpose=False, str
     hd, dev, dtype, n = rot.head_dim, q.device, q.dtype, q.shape[0]
     if dtype not in _ROW_TYPES:
         raise ValueError("q must be float32 or bfloat16")
-    with _Call(dev, stream) as call:
-        made = made_k = None
-        if out is None:
-            out = made = torch.empty(q.shape, dtype=dtype, device=dev)
-        elif out.shape != q.shape:
-            raise ValueError("out must have q's shape")
-        qr, outr = _rows(q, "q", hd, dtype, dev, n), _rows(out, "out", hd, dtype, dev, n)
-        kr = k_outr = None
-        if k is not None:
-            if k_out is None:
-                k_out = made_k = torch.empty(k.shape, dtype=dtype, device=dev)
-            elif k_out.shape != k.shape:
-                raise ValueError("k_out must have k's shape")
-            kr, k_outr = _rows(k, "k", hd, dtype, dev, n), _rows(k_out, "k_out", hd, dtype, dev, n)
-        _check(binding.load().sp_probe_rotary(rot, _ROW_TYPES[dtype], 1 if transpose else 0, n,
-                                              _ids(positions, "positions", n, dev), qr, outr, kr, k_outr, call.stream),
-               "sp_probe_rotary")
-        call.hold(made, made_k)
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return rotary(rot, positions, q, k, out, k_out, transpose, stream)
+    made = made_k = None
+    if out is None:
+        out = made = torch.empty_like(q, memory_format=torch.contiguous_format)
+    elif out.shape != q.shape:
+        raise ValueError("out must have q's shape")
+    qr, outr = _rows(q, "q", hd, dtype, dev, n), _rows(out, "out", hd, dtype, dev, n)
+    kr = k_outr = None
+    if k is not None:
+        if k_out is None:
+            k_out = made_k = torch.empty_like(k, memory_format=torch.contiguous_format)
+        elif k_out.shape != k.shape:
+            raise ValueError("k_out must have k's shape")
+        kr, k_outr = _rows(k, "k", hd, dtype, dev, n), _rows(k_out, "k_out", hd, dtype, dev, n)
+    _check(binding.load().sp_probe_rotary(rot, _ROW_TYPES[dtype], 1 if transpose else 0, n,
+                                          _ids(positions, "positions", n, dev), qr, outr, kr, k_outr,
+                                          _current_stream(_current_device()) if stream is None else stream),
+           "sp_probe_rotary")
+    _hold(stream, dev, made, made_k)
     return out if k is None else (out, k_out)
 
 
@@ -220,12 +213,14 @@ def cache_write(cache: PagedCache, seq_ids, positions, k, v, src_rows=None, rota
     n_src = k.shape[0]
     if src_rows is None and n_src != n:
         raise ValueError(f"k must have {n} rows")
-    with _Call(dev, stream) as call:
-        _check(binding.load().sp_probe_cache_write(
-            cache.c, cache.table, _ROW_TYPES[dtype], n, _ids(seq_ids, "seq_ids", n, dev),
-            _ids(positions, "positions", n, dev), None if src_rows is None else _ids(src_rows, "src_rows", n, dev),
-            n_src, _rows(k, "k", hd, dtype, dev), _rows(v, "v", hd, dtype, dev, n_src), rotary, call.stream),
-            "sp_probe_cache_write")
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return cache_write(cache, seq_ids, positions, k, v, src_rows, rotary, stream)
+    _check(binding.load().sp_probe_cache_write(
+        cache.c, cache.table, _ROW_TYPES[dtype], n, _ids(seq_ids, "seq_ids", n, dev),
+        _ids(positions, "positions", n, dev), None if src_rows is None else _ids(src_rows, "src_rows", n, dev),
+        n_src, _rows(k, "k", hd, dtype, dev), _rows(v, "v", hd, dtype, dev, n_src), rotary,
+        _current_stream(_current_device()) if stream is None else stream), "sp_probe_cache_write")
 
 
 def cache_read(cache: PagedCache, seq_ids, positions, dtype=torch.bfloat16, k=None, v=None, stream=None):
@@ -233,21 +228,23 @@ def cache_read(cache: PagedCache, seq_ids, positions, dtype=torch.bfloat16, k=No
     dtype; given k and v (either or both) are written instead: rows with ids or positions out
     of range are left as they are."""
     dev, n, hd = cache.device, seq_ids.shape[0], cache.head_dim
-    with _Call(dev, stream) as call:
-        made_k = made_v = None
-        if k is None and v is None:
-            shape = (n, cache.n_kv_heads, hd)
-            k = made_k = torch.empty(shape, dtype=dtype, device=dev)
-            v = made_v = torch.empty(shape, dtype=dtype, device=dev)
-        else:
-            dtype = k.dtype if k is not None else v.dtype
-        if dtype not in _ROW_TYPES:
-            raise ValueError("rows must be float32 or bfloat16")
-        _check(binding.load().sp_probe_cache_read(
-            cache.c, cache.table, _ROW_TYPES[dtype], n, _ids(seq_ids, "seq_ids", n, dev),
-            _ids(positions, "positions", n, dev), None if k is None else _rows(k, "k", hd, dtype, dev, n),
-            None if v is None else _rows(v, "v", hd, dtype, dev, n), call.stream), "sp_probe_cache_read")
-        call.hold(made_k, made_v)
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return cache_read(cache, seq_ids, positions, dtype, k, v, stream)
+    made_k = made_v = None
+    if k is None and v is None:
+        k = made_k = torch.empty((n, cache.n_kv_heads, hd), dtype=dtype, device=dev)
+        v = made_v = torch.empty_like(k)
+    else:
+        dtype = k.dtype if k is not None else v.dtype
+    if dtype not in _ROW_TYPES:
+        raise ValueError("rows must be float32 or bfloat16")
+    _check(binding.load().sp_probe_cache_read(
+        cache.c, cache.table, _ROW_TYPES[dtype], n, _ids(seq_ids, "seq_ids", n, dev),
+        _ids(positions, "positions", n, dev), None if k is None else _rows(k, "k", hd, dtype, dev, n),
+        None if v is None else _rows(v, "v", hd, dtype, dev, n),
+        _current_stream(_current_device()) if stream is None else stream), "sp_probe_cache_read")
+    _hold(stream, dev, made_k, made_v)
     return k, v
 
 
@@ -301,36 +298,40 @@ def tree_attention(cache: PagedCache, seq_lens, q, k, v, mask=None, counts=None,
         scale = 0.0
     elif not (math.isfinite(scale) and scale > 0):
         raise ValueError("scale must be positive")
-    with _Call(dev, stream) as call:
-        made = made_ws = None
-        if out is None:
-            out = made = torch.empty(shape, dtype=dtype, device=dev)
-        elif out.shape != shape:
-            raise ValueError("out must have q's shape")
-        tree = binding.sp_tree(nodes, 0, None if counts is None else _ids(counts, "counts", batch, dev), None, 0,
-                               _rows(q, "q", hd, dtype, dev), _rows(k, "k", hd, dtype, dev),
-                               _rows(v, "v", hd, dtype, dev), _rows(out, "out", hd, dtype, dev), None)
-        if mask is not None:
-            words = mask.shape
-            if (mask.dtype not in _MASK_TYPES or mask.device != dev or not mask.is_contiguous()
-                    or not 2 <= len(words) <= 3 or words[-2] != nodes or (len(words) == 3 and words[0] != batch)):
-                raise ValueError("mask must be contiguous int32 words [batch, nodes, words] or [nodes, words]")
-            tree.mask, tree.mask_words = mask.data_ptr(), words[-1]
-            tree.mask_stride = 0 if len(words) == 2 else nodes * words[-1]
-        if lse is not None:
-            if lse.dtype != torch.float32 or lse.device != dev or not lse.is_contiguous() or lse.shape != shape[:3]:
-                raise ValueError("lse must be contiguous float32 [batch, nodes, n_q_heads]")
-            tree.lse = lse.data_ptr()
-        cfg = _tree_config(cache, nq, dtype, nodes, batch or 1, max_seq_len, scale)
-        lib = binding.load()
-        if workspace is None:
-            workspace = made_ws = torch.empty(max(lib.sp_probe_tree_workspace_bytes(cfg), 16), dtype=torch.uint8, device=dev)
-        elif workspace.dtype != torch.uint8 or workspace.device != dev or not workspace.is_contiguous():
-            raise ValueError(f"workspace must be contiguous uint8 on {dev}")
-        _check(lib.sp_probe_tree_attention(cfg, cache.c, _ids(seq_lens, "seq_lens", batch, dev), cache.table, tree,
-                                           workspace.data_ptr(), workspace.numel(), call.stream),
-               "sp_probe_tree_attention")
-        call.hold(made, made_ws)
+    if _elsewhere(dev):
+        with torch.cuda.device(dev):
+            return tree_attention(cache, seq_lens, q, k, v, mask, counts, max_seq_len, scale or None, out, lse, workspace,
+                                  stream)
+    made = made_ws = None
+    if out is None:
+        out = made = torch.empty_like(q, memory_format=torch.contiguous_format)
+    elif out.shape != shape:
+        raise ValueError("out must have q's shape")
+    tree = binding.sp_tree(nodes, 0, None if counts is None else _ids(counts, "counts", batch, dev), None, 0,
+                           _rows(q, "q", hd, dtype, dev), _rows(k, "k", hd, dtype, dev),
+                           _rows(v, "v", hd, dtype, dev), _rows(out, "out", hd, dtype, dev), None)
+    if mask is not None:
+        words = mask.shape
+        if (mask.dtype not in _MASK_TYPES or mask.device != dev or not mask.is_contiguous()
+                or not 2 <= len(words) <= 3 or words[-2] != nodes or (len(words) == 3 and words[0] != batch)):
+            raise ValueError("mask must be contiguous int32 words [batch, nodes, words] or [nodes, words]")
+        tree.mask, tree.mask_words = mask.data_ptr(), words[-1]
+        tree.mask_stride = 0 if len(words) == 2 else nodes * words[-1]
+    if lse is not None:
+        if lse.dtype != torch.float32 or lse.device != dev or not lse.is_contiguous() or lse.shape != shape[:3]:
+            raise ValueError("lse must be contiguous float32 [batch, nodes, n_q_heads]")
+        tree.lse = lse.data_ptr()
+    cfg = _tree_config(cache, nq, dtype, nodes, batch or 1, max_seq_len, scale)
+    lib = binding.load()
+    if workspace is None:
+        workspace = made_ws = torch.empty(max(lib.sp_probe_tree_workspace_bytes(cfg), 16), dtype=torch.uint8, device=dev)
+    elif workspace.dtype != torch.uint8 or workspace.device != dev or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be contiguous uint8 on {dev}")
+    _check(lib.sp_probe_tree_attention(cfg, cache.c, _ids(seq_lens, "seq_lens", batch, dev), cache.table, tree,
+                                       workspace.data_ptr(), workspace.numel(),
+                                       _current_stream(_current_device()) if stream is None else stream),
+           "sp_probe_tree_attention")
+    _hold(stream, dev, made, made_ws)
     return out
 
 
