@@ -1,0 +1,176 @@
+"""Tree attention over the launch plans that small calls do not reach: splits of many windows of
+block ids, more splits than one round of the join, more sequences than the work items' scan
+takes, contiguous storage; and seeded random shapes of all the cache operators."""
+from __future__ import annotations
+
+import math
+
+import pytest
+import torch
+
+from paper_2608_28099_amd import binding, ops
+from tests.test_gpu_ops import STORES, Tree, make_cache, seeded, tokens, words_of
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def dev():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    binding.load()
+    return torch.device("cuda:0")
+
+
+def run(c, **kw):
+    q, k, v = c.qkv()
+    lse = torch.zeros((len(c.lens), c.t, c.nq), device=c.dev)
+    out = ops.tree_attention(c.cache, c.seq_lens, q, k, v, mask=words_of(c.see).to(c.dev), lse=lse,
+                             max_seq_len=max(c.lens), **kw)
+    return out, lse
+
+
+@pytest.mark.parametrize("store", [torch.bfloat16, torch.float8_e4m3fn])
+@pytest.mark.parametrize("contiguous", [False, True])
+def test_splits_of_more_block_ids_than_are_held_at_once(dev, store, contiguous):
+    """131072 tokens in blocks of 16, splits of 16384 (1024 ids, four windows of 256)."""
+    lens = (131072, 40) if contiguous else (131072, 40, 3, 17000, 0, 9, 1, 64, 5, 7, 8, 2)
+    nkv = 48 if contiguous else 8
+    c = Tree(dev, store, lens, 1, nkv, nkv, 64, 16, seed=61, contiguous=contiguous)
+    out, lse = run(c)
+    # every sequence but the longest whole, of the longest the first and last heads
+    c.check(out, lse, sequences=range(1, len(lens)))
+    from oracle import cacheops as oracle
+    from tests.test_gpu_ops import dense
+    kc, vc = dense(c.cache, 0, lens[0])
+    for g in (0, nkv - 1):
+        x = c.x[0]
+        ref, rl, mag, big = oracle.tree_attention(x[:, g:g + 1], kc[g:g + 1], vc[g:g + 1], x[:, nkv + g:nkv + g + 1],
+                                                  x[:, 2 * nkv + g:2 * nkv + g + 1], c.see[0])
+        # as Tree.check: a weight's rounding, the result's, the scores', and sums of n terms (in splits of 16384,
+        # eight of which are joined)
+        eps = 2 * (64 * 2.0 ** -24 * big + 2.0 ** -22) + 2 * 16400 * 2.0 ** -24
+        tol = mag * (2.0 ** -8 + eps) + 2.0 ** -8 * ref.abs()
+        assert torch.all((out[0, :, g:g + 1].cpu().double() - ref).abs() <= tol)
+        assert torch.all((lse[0, :, g:g + 1].cpu().double() - rl).abs() <= eps + 2.0 ** -22 * (1 + rl.abs()))
+
+
+@pytest.mark.parametrize("store", STORES)
+@pytest.mark.parametrize("hd,nodes", [(64, 3), (128, 20)])
+def test_more_splits_than_one_round_of_the_join(dev, store, hd, nodes):
+    """One sequence of 20000 tokens, two KV heads: about 79 splits of 256."""
+    c = Tree(dev, store, (20000,), nodes, 4, 2, hd, 16, seed=62)
+    c.check(*run(c))
+
+
+@pytest.mark.parametrize("store", STORES)
+@pytest.mark.parametrize("batch", [64, 65, 1024, 1100])
+def test_many_sequences(dev, store, batch):
+    """Around the 64 sequences that one step of the work items' scan takes and the 1024 that it takes at all;
+    lengths of several splits among many short ones."""
+    gen = seeded(batch)
+    lens = [int(x) for x in torch.randint(0, 40, (batch,), generator=gen)]
+    for b in (0, 1, 63, batch // 2, batch - 1):
+        lens[b] = 4100 + b
+    lens[5] = 2048 if batch > 100 else 2049
+    c = Tree(dev, store, lens, 2, 2, 1, 64, 16, seed=63)
+    out, lse = run(c)
+    c.check(out, lse, sequences=[0, 1, 2, 5, 62, 63, 64 % batch, batch // 2, batch - 2, batch - 1])
+    # and every sequence against calls of its own size
+    again = ops.tree_attention(c.cache, c.seq_lens, *c.qkv(), mask=words_of(c.see).to(dev), max_seq_len=c.cache.capacity)
+    assert torch.allclose(out.float(), again.float(), rtol=2.0 ** -6, atol=1e-4)
+
+
+@pytest.mark.parametrize("store", STORES)
+def test_the_same_call_under_two_bounds_of_the_length(dev, store):
+    """Splits change with max_seq_len, results only by roundings; a bound below a length clamps it."""
+    c = Tree(dev, store, (3000, 700, 0), 5, 8, 2, 128, 16, seed=64)
+    a, _ = run(c)
+    q, k, v = c.qkv()
+    m = words_of(c.see).to(dev)
+    b = ops.tree_attention(c.cache, c.seq_lens, q, k, v, mask=m)
+    assert torch.allclose(a.float(), b.float(), rtol=2.0 ** -6, atol=1e-4)
+    short = ops.tree_attention(c.cache, c.seq_lens, q, k, v, mask=m, max_seq_len=700)
+    same = ops.tree_attention(c.cache, torch.clamp(c.seq_lens, max=700), q, k, v, mask=m, max_seq_len=700)
+    assert torch.equal(short, same)
+
+
+def test_two_streams_and_a_workspace_of_the_callers(dev):
+    """Overlapping calls with memory of their own, and one after the other on one workspace full of NaN."""
+    c = Tree(dev, torch.bfloat16, (5000, 900), 17, 8, 2, 128, 16, seed=65)
+    ref, _ = run(c)
+    q, k, v = c.qkv()
+    m = words_of(c.see).to(dev)
+    call = lambda **kw: ops.tree_attention(c.cache, c.seq_lens, q, k, v, mask=m, max_seq_len=5000, **kw)  # noqa: E731
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    outs = []
+    for i in range(12):
+        with torch.cuda.stream(streams[i % 3]):
+            outs.append(call())
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, ref) for o in outs)
+    n = ops.tree_workspace_bytes(c.cache, 8, torch.bfloat16, 17, max_seq_len=5000)
+    ws = torch.empty(n, dtype=torch.uint8, device=dev)
+    ws.view(torch.float32).fill_(math.nan)
+    assert torch.equal(call(workspace=ws), ref) and torch.equal(call(workspace=ws), ref)
+    with pytest.raises(binding.ProbeError):
+        call(workspace=ws[:n - 256])
+    # a workspace for larger calls serves smaller ones
+    n2 = ops.tree_workspace_bytes(c.cache, 8, torch.bfloat16, 256)
+    assert n2 >= n and torch.equal(call(workspace=torch.empty(n2, dtype=torch.uint8, device=dev)), ref)
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_random_trees(dev, seed):
+    gen = seeded(1000 + seed)
+    pick = lambda *xs: xs[int(torch.randint(0, len(xs), (1,), generator=gen))]  # noqa: E731
+    hd, nkv, group = pick(64, 128), pick(1, 2, 3), pick(1, 2, 4, 5, 7)
+    t, block, batch = pick(1, 2, 7, 16, 31, 33, 65), pick(16, 32, 64, 128), pick(1, 2, 5)
+    hi = pick(1, 40, 300, 2500)
+    lens = [int(x) for x in torch.randint(0, hi + 1, (batch,), generator=gen)]
+    store = pick(*STORES)
+    print(f"[tree] seed {seed}: {store} lens {lens} nodes {t} heads {nkv}x{group} hd {hd} block {block}", flush=True)
+    c = Tree(dev, store, lens, t, nkv * group, nkv, hd, block, seed=seed, contiguous=pick(False, False, True))
+    see = c.see & (torch.rand(c.see.shape, generator=gen) < pick(1.0, 0.6))
+    counts = [int(x) for x in torch.randint(0, t + 1, (batch,), generator=gen)]
+    q, k, v = c.qkv()
+    out = torch.full(q.shape, 3.0, dtype=c.dtype, device=dev)
+    lse = torch.full(q.shape[:3], 3.0, device=dev)
+    ops.tree_attention(c.cache, c.seq_lens, q, k, v, mask=words_of(see).to(dev), out=out, lse=lse,
+                       counts=torch.tensor(counts, dtype=torch.int32, device=dev))
+    c.check(out, lse, see=see, counts=counts)
+    for b, n in enumerate(counts):
+        assert torch.all(out[b, n:] == 3.0) and torch.all(lse[b, n:] == 3.0)
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_random_rows_in_and_out_of_a_cache(dev, seed):
+    """Rows of several sequences in runs that start anywhere, some reversed, some scattered."""
+    gen = seeded(2000 + seed)
+    pick = lambda *xs: xs[int(torch.randint(0, len(xs), (1,), generator=gen))]  # noqa: E731
+    store, dtype = pick(*STORES), pick(torch.float32, torch.bfloat16)
+    hd, nkv, block = pick(64, 128), pick(1, 2, 5), pick(16, 32, 128)
+    starts = [int(x) for x in torch.randint(0, 70, (4,), generator=gen)]
+    lens = [int(x) for x in torch.randint(0, 150, (4,), generator=gen)]
+    print(f"[rows] seed {seed}: {store} {dtype} hd {hd} block {block} starts {starts} lens {lens}", flush=True)
+    cache = make_cache(dev, store, [a + b for a, b in zip(starts, lens)], nkv, hd, block, seed)
+    seq, pos = tokens(lens, starts)
+    n = len(seq)
+    order = torch.arange(n)
+    if seed % 3 == 1:
+        order = order.flip(0)
+    if seed % 3 == 2 and n > 40:
+        order[20:40] = order[20:40][torch.randperm(20, generator=gen)]
+    seq, pos = seq[order].to(dev), pos[order].to(dev)
+    x = torch.randn((n, 2 * nkv, hd), generator=gen).to(dtype).to(dev)
+    if n:
+        ops.cache_write(cache, seq, pos, x[:, :nkv], x[:, nkv:])
+    k, v = ops.cache_read(cache, seq, pos, torch.float32)
+    if store == torch.float8_e4m3fn:
+        from oracle import cacheops as oracle
+        for got, want in ((k, x[:, :nkv]), (v, x[:, nkv:])):
+            val, byte = oracle.quantise(want.cpu())
+            assert torch.equal(got.cpu().double(), val * torch.exp2(byte.double() - 127)[..., None])
+    else:
+        assert torch.equal(k, x[:, :nkv].to(store).float()) and torch.equal(v, x[:, nkv:].to(store).float())
