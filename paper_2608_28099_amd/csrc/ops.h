@@ -58,17 +58,16 @@ struct TreeParams {
   int64_t mask_stride;
   int mask_words;
   RowsArg q, k, v, out;
-  int q_vec, k_vec, v_vec;
+  int q_vec, k_vec, v_vec, o_vec;
   float* lse;                    // nullable
   int nodes, group, max_seq_len;
   float scale_log2;              // the scores' factor times log2(e)
-  // the plan: query rows in n_qgroups groups of 64 (fp32: 16), a workgroup each, r_alloc rows in
-  // all; splits of split_len tokens, max_splits of max_seq_len
-  int n_qgroups, r_alloc, split_len, max_splits;
+  // the plan: query rows in n_qgroups groups, a workgroup each, of four waves of rows_per_wave (16 or
+  // 32; fp32: groups of 16 rows), r_alloc rows in all; splits of split_len tokens, max_splits of max_seq_len
+  int n_qgroups, rows_per_wave, r_alloc, split_len, max_splits;
   float* o_part;                 // [B][n_kv][max_splits][r_alloc / 16][16 hd], not divided by the sum
   float2* ml_part;               // [B][n_kv][max_splits][r_alloc]: maximum (log2 units), sum
 };
-constexpr int kTreeRows = 64, kTreeRowsF32 = 16;  // query rows of a workgroup
 hipError_t launch_tree(const TreeParams& p, int storage, int hd, hipStream_t s);
 
 }  // namespace sp

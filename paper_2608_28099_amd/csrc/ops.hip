@@ -120,14 +120,14 @@ int check_tree_config(const sp_tree_config* c) {
   if (!(c->scale >= 0.f) || !std::isfinite(c->scale)) return SP_ERR_INVALID_ARG;
   if (c->head_dim != 64 && c->head_dim != 128) return SP_ERR_UNSUPPORTED;
   if ((c->dtype == SP_F32) != (c->kv_dtype == SP_F32)) return SP_ERR_UNSUPPORTED;
-  if (c->max_nodes > 256 || c->n_q_heads > 4096 || c->max_batch > 65535) return SP_ERR_UNSUPPORTED;
+  if (c->max_nodes > 256 || c->n_q_heads > 4096 || c->max_batch > 65535 || c->max_seq_len > 1 << 30) return SP_ERR_UNSUPPORTED;
   return SP_OK;
 }
 
 // How a call of `nodes` nodes is laid out on num_cus compute units.  The splits follow the
 // config's max_batch, so that its workspace holds every call's partial results.
 struct TreePlan {
-  int n_qgroups, r_alloc, split_len, max_splits;
+  int n_qgroups, rows_per_wave, r_alloc, split_len, max_splits;
   size_t part_bytes;  // of O; the (m, l) pairs follow
   size_t total;
 };
@@ -135,14 +135,31 @@ struct TreePlan {
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 constexpr int kMinSplit = 256;  // tokens
+int64_t slots_of(int num_cus) { return (int64_t)num_cus * 3; }  // three workgroups per compute unit, by LDS
+
+// Rows of a wave, and workgroups (of four waves) that the rows of a KV head take; fp32: 16 rows a
+// workgroup.  A wave of 32 rows reads half as much from LDS per row and converts 8-bit keys and values half as often,
+// but one group of 128 rows in place of two of 64 leaves half as many to spread over the device.  So
+// waves of 32 from 129 rows on, where padding to 128 adds at most a fifth and pieces of kMinSplit tokens
+// would still fill the device twice.  Measured (8 KV heads, head dim 128, in us, 16 rows a wave / 32): 64 sequences of 6000
+// tokens, bf16: 240 rows 607 / 533, 320 rows 756 / 684, 480 rows 1113 / 949; 8-bit: 637 / 617, 801 / 805, 1195 / 1117; 160
+// rows, padded to 192 or 256: 487 / 460 and 490 / 517; 16 of 4000, 160 rows: 76 / 86 and 96 / 105, 128 rows: 63 / 77 and
+// 73 / 80; 240 rows, 4 of 8000: 56.6 / 57.3 and 69.6 / 68.0, one of 2000: 20.2 / 23.6 and 20.9 / 26.4.
+void row_groups(const sp_tree_config& c, int nodes, int num_cus, int* rows_per_wave, int* groups) {
+  const int rows = nodes * (c.n_q_heads / c.n_kv_heads), g64 = (rows + 63) / 64, g128 = (rows + 127) / 128;
+  const bool f32 = c.kv_dtype == SP_F32;
+  const int64_t pieces = (int64_t)c.max_batch * c.n_kv_heads * g128 * (c.max_seq_len / kMinSplit);
+  const bool wide = !f32 && rows > 128 && 5 * 128 * g128 <= 6 * 64 * g64 && pieces >= 2 * slots_of(num_cus);
+  *rows_per_wave = wide ? 32 : 16;
+  *groups = f32 ? (rows + 15) / 16 : wide ? g128 : g64;
+}
 
 TreePlan tree_plan(const sp_tree_config& c, int nodes, int num_cus) {
   TreePlan p{};
-  const int rows = nodes * (c.n_q_heads / c.n_kv_heads), per = c.kv_dtype == SP_F32 ? kTreeRowsF32 : kTreeRows;
-  p.n_qgroups = (rows + per - 1) / per;
-  p.r_alloc = p.n_qgroups * per;
+  row_groups(c, nodes, num_cus, &p.rows_per_wave, &p.n_qgroups);
+  p.r_alloc = p.n_qgroups * (c.kv_dtype == SP_F32 ? 16 : 4 * p.rows_per_wave);
   const int64_t items = (int64_t)c.max_batch * c.n_kv_heads * p.n_qgroups;
-  const int64_t n = c.max_seq_len, slots = (int64_t)num_cus * 3;  // three workgroups per compute unit, by LDS
+  const int64_t n = c.max_seq_len, slots = slots_of(num_cus);
   // As many splits as fill the device once, and pieces of at most an eighth of the longest sequence
   // (or 2048 tokens): a batch of long and short sequences takes several rounds, whose ends level
   // out (64 sequences of 2K-32K tokens, 320 rows: 1315-1345 us in splits of 4096-8192, 1655 of 1024,
@@ -173,14 +190,17 @@ TreePlan tree_plan(const sp_tree_config& c, int nodes, int num_cus) {
   return p;
 }
 
-// The largest plan of the calls that c allows: splits change with the number of query groups only,
-// and within one number of groups every plan is alike.
+// The largest plan of the calls that c allows: a plan changes with the groups of rows only.
 size_t tree_workspace(const sp_tree_config& c, int num_cus) {
-  const int group = c.n_q_heads / c.n_kv_heads, per = c.kv_dtype == SP_F32 ? kTreeRowsF32 : kTreeRows;
-  size_t most = tree_plan(c, c.max_nodes, num_cus).total;
-  for (int q = 1; per * q / group < c.max_nodes; ++q) {  // the most nodes of q groups
-    const int nodes = per * q / group;
-    const size_t x = nodes > 0 ? tree_plan(c, nodes, num_cus).total : 0;
+  size_t most = 0;
+  int wave0 = 0, groups0 = 0;
+  for (int nodes = 1; nodes <= c.max_nodes; ++nodes) {
+    int wave, groups;
+    row_groups(c, nodes, num_cus, &wave, &groups);
+    if (wave == wave0 && groups == groups0) continue;
+    wave0 = wave;
+    groups0 = groups;
+    const size_t x = tree_plan(c, nodes, num_cus).total;
     most = x > most ? x : most;
   }
   return most;
@@ -383,6 +403,7 @@ SP_API int sp_probe_tree_attention(const sp_tree_config* c, const sp_kv_store* s
   if (workspace_bytes < pl.total) return SP_ERR_INVALID_ARG;
   if (st != SP_OK) return st;
   p.n_qgroups = pl.n_qgroups;
+  p.rows_per_wave = pl.rows_per_wave;
   p.r_alloc = pl.r_alloc;
   p.split_len = pl.split_len;
   p.max_splits = pl.max_splits;
@@ -401,6 +422,7 @@ SP_API int sp_probe_tree_attention(const sp_tree_config* c, const sp_kv_store* s
   p.q_vec = q_vec;
   p.k_vec = k_vec;
   p.v_vec = v_vec;
+  p.o_vec = o_vec;
   p.lse = t->lse;
   p.nodes = t->n_nodes;
   p.group = c->n_q_heads / c->n_kv_heads;

@@ -2,20 +2,17 @@
 // sp_probe_tree_attention).
 //
 // Query rows of a KV head: row r = i * G + j is node i and the j-th of the G query
-// heads that share it.  A wave takes 16 rows and the tokens of its sequence in units,
-// first the cached ones, then the nodes, with one running softmax per row (maximum m in
-// log2 units, sum l, output O not yet divided by l).
+// heads that share it.  A wave takes 16 or 32 rows and the tokens of its sequence's split in
+// units, first the nodes, then the cached ones, with one running softmax per row (reference
+// maximum m in log2 units, sum l, output O not yet divided by l).
 //
-// Matrix-core operands (bf16 arithmetic).  S^T = K Q^T on 16x16x32 products: lane
-// (li, la) = (lane % 16, lane / 16) holds of K the 8 dims 8 (la NC + c) .. + 7 of one
-// token for product c, and receives the scores of query row li and four tokens.  Product h
-// of a unit takes as its row m the token TPL (m / 4) + 4 h + m % 4, so that the lane's
-// scores over all h are those of the TPL consecutive tokens TPL la .. : exactly its
-// operand of O += P V, whose other operand is those tokens of dim 16 nt + li, side by side
-// in the cache.  TPL is 8 (units of 32 tokens) for bf16 caches and nodes and 16 (units of
-// 64) for 8-bit caches, so that either reads 16 bytes per lane at a time.  8-bit keys become
-// bf16 with their exponent, exactly; the values' exponents go to the weights instead,
-// exactly too (a power of two).
+// Matrix-core operands (bf16 arithmetic): S^T = K Q^T, then O^T += V^T P^T, so that the
+// scores, the sum and the output of a row stay in the lanes of that row, and the scores that a
+// lane receives of the first product are, as weights, its operand of the second.  For that the
+// keys' tokens go to the rows of the first product in an order of their own (Wave16, Wave32).
+// Units: 32 tokens of bf16 caches and nodes, 64 of 8-bit caches, so that either reads 16 bytes
+// per lane at a time.  8-bit keys become bf16 with their exponent, exactly; the values'
+// exponents go to the weights instead, exactly too (a power of two).
 #include <type_traits>
 
 #include "common.h"
@@ -67,69 +64,23 @@ __device__ __forceinline__ float exponent_scale(uint32_t byte) {
   return __builtin_bit_cast(float, byte << 23);
 }
 
-template <int HD>
-struct Rows {  // a wave's 16 query rows
-  static constexpr int NC = HD / 32, NT = HD / 16;
-  bf16x8 q[NC];   // Q[row li][8 (la NC + c) ..]
-  f32x4 o[NT];    // O[row 4 la + r][16 nt + li]
-  float m, l;     // row li: reference maximum (log2 units); the lane's part of the sum
-};
-
 // A row's reference maximum moves only when a score exceeds it by more than this (log2
 // units), so weights stay below 2^8 between moves and most units skip the exchange
 // across lanes and the rescaling of O.
 constexpr float kRescaleLog2 = 8.0f;
 
-// Moves a row's reference maximum (and l and o with it) where one of the lane's scores s (products
-// not yet scaled, masked ones -inf) exceeds it by too much.
-template <int HD, int NH>
-__device__ __forceinline__ void raise_maximum(Rows<HD>& st, const f32x4 (&s)[NH], float scale, int la) {
-  float mx = fmaxf(s[0][0], s[0][1]);
-#pragma unroll
-  for (int i = 2; i < 4 * NH; ++i) mx = fmaxf(mx, s[i / 4][i % 4]);
-  mx *= scale;
-  if (__any(mx > st.m + kRescaleLog2)) {
-    mx = fmaxf(mx, __shfl_xor(mx, 16));
-    mx = fmaxf(mx, __shfl_xor(mx, 32));
-    mx = fmaxf(mx, st.m);
-    const float alpha = fast_exp2(st.m - mx);
-    st.m = mx;
-    st.l *= alpha;
-    float ar[4];  // the factors of this lane's O rows 4 la + r
-#pragma unroll
-    for (int r = 0; r < 4; ++r) ar[r] = __shfl(alpha, 4 * la + r);
-#pragma unroll
-    for (int nt = 0; nt < Rows<HD>::NT; ++nt)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) st.o[nt][r] *= ar[r];
-  }
-}
-
-// The weights of 8 tokens (scores h0 and h0 + 1) as a bf16 operand.  Rounded to nearest:
-// each weight moves by at most 2^-8 of itself, what rounding the result to bf16 may cost too.
-template <int NH>
-__device__ __forceinline__ bf16x8 weights8(const f32x4 (&s)[NH], int h0) {
-  bf16x8 w;
-#pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    w[r] = (bf16)s[h0][r];
-    w[4 + r] = (bf16)s[h0 + 1][r];
-  }
-  return w;
-}
-
 // LDS image of a unit, in 16-byte pieces: NSUB runs of 16 tokens (each inside one
 // block), their keys, then their values.  A run's keys: piece c * 16 + t = 16 bytes of dims
 // of token t; its values: 8-bit: piece d = dim d of its 16 tokens; bf16: piece
-// (2 nt + e) * 16 + i = dim 16 nt + i of its tokens 8 e .. 8 e + 7.  The 4-piece pad between
-// the runs' keys lets the 16 lanes of a key fragment (4 or 8 tokens of every run) hit 16
-// different 16-byte bank groups; a value fragment is 256 bytes in a row per 16 lanes.
+// (2 nt + e) * 16 + i = dim 16 nt + i of its tokens 8 e .. 8 e + 7.  The pad between the runs' keys
+// lets the 16 lanes of a key fragment (4 or 8 tokens of several runs) hit 16 different 16-byte
+// bank groups; a value fragment is 256 bytes in a row per 16 lanes.
 // Pieces go from memory to LDS 64 at a time, each lane its own address.
-template <int HD, bool E8>
+template <int HD, bool E8, int PAD>
 struct Unit {
   static constexpr int NSUB = E8 ? 4 : 2, TOKENS = 16 * NSUB;
   static constexpr int SUB = E8 ? HD : 2 * HD;       // pieces of a run's keys, or of its values
-  static constexpr int KP = SUB + 4, VB = NSUB * KP;
+  static constexpr int KP = SUB + PAD, VB = NSUB * KP;
   static constexpr int EB = VB + NSUB * SUB;         // exponents: per run 4 words the keys', 4 the values'
   static constexpr int PIECES = EB + (E8 ? 2 * NSUB : 0);
   static constexpr int IPG = SUB / 64;               // loads of 64 pieces per run's keys, or its values
@@ -156,104 +107,385 @@ __device__ __forceinline__ uint32_t keep_mask(int keep) {
   return keep >= 4 / E ? ~0u : keep > 0 ? (1u << (8 * E * keep)) - 1 : 0u;
 }
 
-// Scores of a staged unit, not scaled.
+// Eight weights as a bf16 operand.  Rounded to nearest: each moves by at most 2^-8 of itself,
+// what rounding the result to bf16 may cost too.
+__device__ __forceinline__ bf16x8 weights8(const float* s) {
+  bf16x8 w;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w[i] = (bf16)s[i];
+  return w;
+}
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// The softmax and products that both kinds of wave share.  D: the derived wave, with its operands in
+//   q[NC]       queries
+//   o[NO]       O^T: NO vectors of OV values, all of the lane's row
+//   m, l        the row's reference maximum (log2 units); the lane's part of its sum
+// S scores per lane and step (one row, S consecutive or grouped tokens).
+template <int NO, typename OVec, int OV>
+struct RowState {
+  OVec o[NO];
+  float m, l;
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int j = 0; j < NO; ++j)
+#pragma unroll
+      for (int r = 0; r < OV; ++r) o[j][r] = 0.f;
+    m = kNegBig;
+    l = 0.f;
+  }
+  // Moves the reference maximum (and l and O) where one of the lane's scores s (products not yet scaled,
+  // masked ones -inf) exceeds it by too much.  FROM: the first lane bit that tells lanes of a row apart.
+  template <int S, int FROM>
+  __device__ __forceinline__ void raise(const float (&s)[S], float scale) {
+    float mx = fmaxf(s[0], s[1]);
+#pragma unroll
+    for (int i = 2; i < S; ++i) mx = fmaxf(mx, s[i]);
+    mx *= scale;
+    if (__any(mx > m + kRescaleLog2)) {
+#pragma unroll
+      for (int b = FROM; b < 64; b <<= 1) mx = fmaxf(mx, __shfl_xor(mx, b));
+      mx = fmaxf(mx, m);
+      const float alpha = fast_exp2(m - mx);
+      m = mx;
+      l *= alpha;
+#pragma unroll
+      for (int j = 0; j < NO; ++j)
+#pragma unroll
+        for (int r = 0; r < OV; ++r) o[j][r] *= alpha;
+    }
+  }
+  // Scores to weights 2^(s scale - m).
+  template <int S>
+  __device__ __forceinline__ void weigh(float (&s)[S], float scale) {
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+      s[i] = fast_exp2(fmaf(s[i], scale, -m));
+      l += s[i];
+    }
+  }
+};
+
+// A wave of 16 rows on 16x16x32 products.  Lane (li, la) = (lane % 16, lane / 16) belongs to row li and
+// holds of K the dims 8 (la NC + c) .. + 7 of one token for product c.  Product h of a unit takes as
+// its row m the token TPL (m / 4) + 4 h + m % 4, so that the lane's scores over all h are those of the
+// TPL consecutive tokens TPL la ..: its operand of the second product, whose other operand is those
+// tokens of dim 16 nt + li, side by side in the cache (TPL 8 in bf16 units, 16 in 8-bit ones).
 template <int HD, bool E8>
-__device__ __forceinline__ void unit_scores(const Rows<HD>& st, f32x4 (&s)[E8 ? 4 : 2], const u32x4* sb, int li, int la) {
-  using L = Unit<HD, E8>;
-  constexpr int NC = HD / 32, NH = E8 ? 4 : 2, TPL = 4 * NH;
-  const int run = TPL * (li >> 2) / 16, first = TPL * (li >> 2) % 16 + (li & 3);  // of the lane's key
+struct Wave16 {
+  static constexpr int ROWS = 16, PAD = 4, NC = HD / 32, NT = HD / 16;
+  RowState<NT, f32x4, 4> st;  // o[nt][r]: dim 16 nt + 4 la + r
+  bf16x8 q[NC];
+  int li, la;
+  __device__ __forceinline__ Wave16(int lane) : li(lane & 15), la(lane >> 4) { st.clear(); }
+  __device__ __forceinline__ int row() const { return li; }
+  __device__ __forceinline__ void load_queries(const bf16* p, bool vec) {
 #pragma unroll
-  for (int h = 0; h < NH; ++h) s[h] = f32x4{0.f, 0.f, 0.f, 0.f};
-  if constexpr (E8) {
-    const u32x4 ek = sb[L::EB + 2 * run];
+    for (int c = 0; c < NC; ++c) q[c] = __builtin_bit_cast(bf16x8, row8(p + 8 * (la * NC + c), vec));
+  }
+
+  template <bool U8>
+  __device__ __forceinline__ void scores(float (&s)[U8 ? 16 : 8], const u32x4* sb) const {
+    using L = Unit<HD, U8, PAD>;
+    constexpr int NH = U8 ? 4 : 2, TPL = 4 * NH;
+    const int run = TPL * (li >> 2) / 16, first = TPL * (li >> 2) % 16 + (li & 3);  // of the lane's key
+    f32x4 d[NH];
 #pragma unroll
-    for (int h = 0; h < NH; ++h) {
-      const float f = exponent_scale((ek[h] >> (8 * (li & 3))) & 0xffu);
+    for (int h = 0; h < NH; ++h) d[h] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if constexpr (U8) {
+      const u32x4 ek = sb[L::EB + 2 * run];
 #pragma unroll
-      for (int q = 0; q < NC / 2; ++q) {
-        const u32x4 w = sb[run * L::KP + (la * (NC / 2) + q) * 16 + first + 4 * h];
-        s[h] = mfma16x16x32_bf16(from_e4m3(w[0], w[1], f), st.q[2 * q], s[h]);
-        s[h] = mfma16x16x32_bf16(from_e4m3(w[2], w[3], f), st.q[2 * q + 1], s[h]);
+      for (int h = 0; h < NH; ++h) {
+        const float f = exponent_scale((ek[h] >> (8 * (li & 3))) & 0xffu);
+#pragma unroll
+        for (int c = 0; c < NC / 2; ++c) {
+          const u32x4 w = sb[run * L::KP + (la * (NC / 2) + c) * 16 + first + 4 * h];
+          d[h] = mfma16x16x32_bf16(from_e4m3(w[0], w[1], f), q[2 * c], d[h]);
+          d[h] = mfma16x16x32_bf16(from_e4m3(w[2], w[3], f), q[2 * c + 1], d[h]);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int h = 0; h < NH; ++h)
+          d[h] = mfma16x16x32_bf16(__builtin_bit_cast(bf16x8, sb[run * L::KP + (la * NC + c) * 16 + first + 4 * h]), q[c], d[h]);
+    }
+#pragma unroll
+    for (int i = 0; i < TPL; ++i) s[i] = d[i / 4][i % 4];
+  }
+
+  // Scores, weights and values of a staged unit of cached tokens; in a tail `limit` tokens of it exist, the
+  // rest may hold anything.
+  __device__ __forceinline__ void cached_unit(const u32x4* sb, bool tail, int limit, float scale) {
+    using L = Unit<HD, E8, PAD>;
+    constexpr int TPL = E8 ? 16 : 8;
+    float s[TPL];
+    scores<E8>(s, sb);
+    // values are read once the scores' products are issued, into registers the keys held
+    __builtin_amdgcn_sched_barrier(0);
+    u32x4 v[NT], e = u32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+      v[nt] = E8 ? sb[L::VB + la * L::SUB + 16 * nt + li] : sb[L::VB + (la >> 1) * L::SUB + (2 * nt + (la & 1)) * 16 + li];
+    if constexpr (E8) e = sb[L::EB + 2 * la + 1];
+    if (tail) {
+      int lim = limit;
+      asm volatile("" : "+s"(lim));  // (keeps the masks a branch that whole units skip)
+#pragma unroll
+      for (int i = 0; i < TPL; ++i)
+        if (TPL * la + i >= lim) s[i] = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const uint32_t keep = E8 ? keep_mask<1>(lim - (16 * la + 4 * w)) : keep_mask<2>(lim - (8 * la + 2 * w));
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) v[nt][w] &= keep;
+        e[w] &= keep;
       }
     }
-  } else {
+    st.template raise<TPL, 16>(s, scale);
+    st.weigh(s, scale);
+    if constexpr (E8) {
 #pragma unroll
-    for (int q = 0; q < NC; ++q)
+      for (int i = 0; i < TPL; ++i) s[i] *= exponent_scale((e[i / 4] >> (8 * (i % 4))) & 0xffu);
+      const bf16x8 p0 = weights8(s), p1 = weights8(s + 8);
 #pragma unroll
-      for (int h = 0; h < NH; ++h)
-        s[h] = mfma16x16x32_bf16(__builtin_bit_cast(bf16x8, sb[run * L::KP + (la * NC + q) * 16 + first + 4 * h]),
-                                 st.q[q], s[h]);
+      for (int nt = 0; nt < NT; ++nt) {
+        st.o[nt] = mfma16x16x32_bf16(from_e4m3(v[nt][0], v[nt][1], 1.f), p0, st.o[nt]);
+        st.o[nt] = mfma16x16x32_bf16(from_e4m3(v[nt][2], v[nt][3], 1.f), p1, st.o[nt]);
+      }
+    } else {
+      const bf16x8 p0 = weights8(s);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) st.o[nt] = mfma16x16x32_bf16(__builtin_bit_cast(bf16x8, v[nt]), p0, st.o[nt]);
+    }
   }
-}
 
-// Tokens at or past `limit` of the lane's scores become -inf.
-template <int NH>
-__device__ __forceinline__ void mask_tail(f32x4 (&s)[NH], int limit, int la) {
+  // A staged unit of nodes, of which the lane's row sees those in `seen`.  odd(t, weight): called for every
+  // node t that may hold values that are not finite, with the row's weight for it, if any_odd.
+  template <typename F>
+  __device__ __forceinline__ void node_unit(const u32x4* sb, uint32_t seen, float scale, bool any_odd, F odd) {
+    using L = Unit<HD, false, PAD>;
+    float s[8];
+    scores<false>(s, sb);
 #pragma unroll
-  for (int i = 0; i < 4 * NH; ++i)
-    if (4 * NH * la + i >= limit) s[i / 4][i % 4] = -INFINITY;
-}
+    for (int i = 0; i < 8; ++i)
+      if (!((seen >> (8 * la + i)) & 1)) s[i] = -INFINITY;
+    st.template raise<8, 16>(s, scale);
+    st.weigh(s, scale);
+    const bf16x8 p0 = weights8(s);
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+      st.o[nt] = mfma16x16x32_bf16(
+          __builtin_bit_cast(bf16x8, sb[L::VB + (la >> 1) * L::SUB + (2 * nt + (la & 1)) * 16 + li]), p0, st.o[nt]);
+    if (any_odd)
+      for (int t = 0; t < 32; ++t) {
+        float w = (float)p0[0];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) w = (t & 7) == i ? (float)p0[i] : w;
+        odd(t, __shfl(w, 16 * (t >> 3) + li));
+      }
+  }
 
-// The lane's fragments of a staged unit's values, and their exponents.  Tokens at or past `limit`
-// may hold anything and become 0.
-template <int HD, bool E8>
-struct Values {
-  u32x4 v[HD / 16], e;
+  __device__ __forceinline__ float sum() const {
+    float l = st.l;
+    l += __shfl_xor(l, 16);
+    return l + __shfl_xor(l, 32);
+  }
+  // f(first dim of four, the four values)
+  template <typename F>
+  __device__ __forceinline__ void each4(F f) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) f(16 * nt + 4 * la, st.o[nt]);
+  }
+  template <typename F>
+  __device__ __forceinline__ void add4(F f) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) st.o[nt][r] = f(16 * nt + 4 * la + r, st.o[nt][r]);
+  }
 };
-template <int HD, bool E8>
-__device__ __forceinline__ void read_values(Values<HD, E8>& x, const u32x4* sb, int li, int la) {
-  using L = Unit<HD, E8>;
-#pragma unroll
-  for (int nt = 0; nt < HD / 16; ++nt)
-    x.v[nt] = E8 ? sb[L::VB + la * L::SUB + 16 * nt + li]
-                 : sb[L::VB + (la >> 1) * L::SUB + (2 * nt + (la & 1)) * 16 + li];
-  if constexpr (E8) x.e = sb[L::EB + 2 * la + 1];
-}
-template <int HD, bool E8>
-__device__ __forceinline__ void clear_tail(Values<HD, E8>& x, int limit, int la) {
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    const uint32_t keep = E8 ? keep_mask<1>(limit - (16 * la + 4 * w)) : keep_mask<2>(limit - (8 * la + 2 * w));
-#pragma unroll
-    for (int nt = 0; nt < HD / 16; ++nt) x.v[nt][w] &= keep;
-    if constexpr (E8) x.e[w] &= keep;
-  }
-}
 
-// The scores become weights 2^(s scale - m), and the values are added with them.  weights: of bf16 units.
+// A wave of 32 rows on 32x32x16 products: each fragment that it reads from LDS serves twice the rows.
+// Lane (lj, lh) = (lane % 32, lane / 32) belongs to row lj.  bf16 units: row m of the first product is
+// token 16 (m / 16) + 8 (m / 4 % 2) + 4 (m / 8 % 2) + m % 4, so that score i of the lane is token
+// 16 (i / 8) + 8 lh + i % 8: eight tokens of each run.  8-bit units, 32 tokens (two runs) at a time: row m is
+// token m % 4 + 4 (m / 8) of run m / 4 % 2, so that the lane's 16 scores are those of run lh.
 template <int HD, bool E8>
-__device__ __forceinline__ void add_values(Rows<HD>& st, f32x4 (&s)[E8 ? 4 : 2], const Values<HD, E8>& x, bf16x8& weights,
-                                           float scale) {
-  constexpr int NT = HD / 16, NH = E8 ? 4 : 2;
+struct Wave32 {
+  static constexpr int ROWS = 32, PAD = 8, NC = HD / 16, ND = HD / 32;
+  RowState<ND, f32x16, 16> st;  // o[dt][4 k + r]: dim 32 dt + 8 k + 4 lh + r
+  bf16x8 q[NC];
+  int lj, lh;
+  __device__ __forceinline__ Wave32(int lane) : lj(lane & 31), lh(lane >> 5) { st.clear(); }
+  __device__ __forceinline__ int row() const { return lj; }
+  // product c takes dims 8 (2 c + lh) .. (bf16 keys), or with 8-bit keys, whose 16 bytes hold 16 dims, the half
+  // c % 2 of piece 2 (c / 2) + lh; the nodes' products follow the same order
+  __device__ __forceinline__ int dims(int c) const { return E8 ? 16 * (2 * (c / 2) + lh) + 8 * (c % 2) : 8 * (2 * c + lh); }
+  __device__ __forceinline__ void load_queries(const bf16* p, bool vec) {
 #pragma unroll
-  for (int h = 0; h < NH; ++h)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      s[h][r] = fast_exp2(fmaf(s[h][r], scale, -st.m));
-      st.l += s[h][r];
-      if constexpr (E8) s[h][r] *= exponent_scale((x.e[h] >> (8 * r)) & 0xffu);
-    }
-  const bf16x8 p0 = weights8(s, 0);
-  if constexpr (E8) {
-    const bf16x8 p1 = weights8(s, 2);
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      st.o[nt] = mfma16x16x32_bf16(p0, from_e4m3(x.v[nt][0], x.v[nt][1], 1.f), st.o[nt]);
-      st.o[nt] = mfma16x16x32_bf16(p1, from_e4m3(x.v[nt][2], x.v[nt][3], 1.f), st.o[nt]);
-    }
-  } else {
-    weights = p0;
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) st.o[nt] = mfma16x16x32_bf16(p0, __builtin_bit_cast(bf16x8, x.v[nt]), st.o[nt]);
+    for (int c = 0; c < NC; ++c) q[c] = __builtin_bit_cast(bf16x8, row8(p + dims(c), vec));
   }
-}
+  static __device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+  }
+
+  __device__ __forceinline__ void bf16_scores(float (&s)[16], const u32x4* sb) const {
+    using L = Unit<HD, false, PAD>;
+    const int at = (lj >> 4) * L::KP + 8 * ((lj >> 2) & 1) + 4 * ((lj >> 3) & 1) + (lj & 3);
+    f32x16 d;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) d[i] = 0.f;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) d = mfma(__builtin_bit_cast(bf16x8, sb[at + dims(c) / 8 * 16]), q[c], d);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = d[i];
+  }
+  // the value fragment of dim tile dt and eight of the tokens of run t
+  __device__ __forceinline__ u32x4 bf16_values(const u32x4* sb, int dt, int t) const {
+    using L = Unit<HD, false, PAD>;
+    return sb[L::VB + t * L::SUB + (2 * (2 * dt + (lj >> 4)) + lh) * 16 + (lj & 15)];
+  }
+
+  // keeps the first `keep` of the fragments' eight tokens
+  static __device__ __forceinline__ void clear_tail(u32x4 (&v)[ND], int keep) {
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const uint32_t bits = keep_mask<2>(keep - 2 * w);
+#pragma unroll
+      for (int dt = 0; dt < ND; ++dt) v[dt][w] &= bits;
+    }
+  }
+
+  __device__ __forceinline__ void cached_unit(const u32x4* sb, bool tail, int limit, float scale) {
+    using L = Unit<HD, E8, PAD>;
+    float s[16];
+    if constexpr (!E8) {
+      bf16_scores(s, sb);
+      __builtin_amdgcn_sched_barrier(0);
+      u32x4 v[ND];
+#pragma unroll
+      for (int dt = 0; dt < ND; ++dt) v[dt] = bf16_values(sb, dt, 0);
+      if (tail) {
+        int lim = limit;
+        asm volatile("" : "+s"(lim));  // (keeps the masks a branch that whole units skip)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (16 * (i / 8) + 8 * lh + i % 8 >= lim) s[i] = -INFINITY;
+        clear_tail(v, lim - 8 * lh);
+      }
+      st.template raise<16, 32>(s, scale);
+      st.weigh(s, scale);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const bf16x8 p = weights8(s + 8 * t);
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt) st.o[dt] = mfma(__builtin_bit_cast(bf16x8, v[dt]), p, st.o[dt]);
+        if (t) break;
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt) v[dt] = bf16_values(sb, dt, 1);
+        if (tail) clear_tail(v, limit - 16 - 8 * lh);
+      }
+    } else {
+#pragma unroll
+      for (int w2 = 0; w2 < 2; ++w2) {
+        if (tail && 32 * w2 >= limit) break;
+        const int run = 2 * w2 + ((lj >> 2) & 1), slot = (lj & 3) + 4 * (lj >> 3);
+        const uint32_t ek = ((const uint32_t*)&sb[L::EB + 2 * run])[slot >> 2];
+        const float f = exponent_scale((ek >> (8 * (slot & 3))) & 0xffu);
+        f32x16 d;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) d[i] = 0.f;
+#pragma unroll
+        for (int c = 0; c < NC / 2; ++c) {
+          const u32x4 w = sb[run * L::KP + (2 * c + lh) * 16 + slot];
+          d = mfma(from_e4m3(w[0], w[1], f), q[2 * c], d);
+          d = mfma(from_e4m3(w[2], w[3], f), q[2 * c + 1], d);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = d[i];
+        __builtin_amdgcn_sched_barrier(0);
+        const int vrun = 2 * w2 + lh;  // the run of the lane's weights
+        u32x4 v[ND], e = sb[L::EB + 2 * vrun + 1];
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt) v[dt] = sb[L::VB + vrun * L::SUB + 32 * dt + lj];
+        if (tail) {
+          int lim = limit;
+          asm volatile("" : "+s"(lim));
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (16 * vrun + i >= lim) s[i] = -INFINITY;
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const uint32_t keep = keep_mask<1>(lim - (16 * vrun + 4 * w));
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt) v[dt][w] &= keep;
+            e[w] &= keep;
+          }
+        }
+        st.template raise<16, 32>(s, scale);
+        st.weigh(s, scale);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] *= exponent_scale((e[i / 4] >> (8 * (i % 4))) & 0xffu);
+        const bf16x8 p0 = weights8(s), p1 = weights8(s + 8);
+#pragma unroll
+        for (int dt = 0; dt < ND; ++dt) {
+          st.o[dt] = mfma(from_e4m3(v[dt][0], v[dt][1], 1.f), p0, st.o[dt]);
+          st.o[dt] = mfma(from_e4m3(v[dt][2], v[dt][3], 1.f), p1, st.o[dt]);
+        }
+      }
+    }
+  }
+
+  template <typename F>
+  __device__ __forceinline__ void node_unit(const u32x4* sb, uint32_t seen, float scale, bool any_odd, F odd) {
+    float s[16];
+    bf16_scores(s, sb);
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (!((seen >> (16 * (i / 8) + 8 * lh + i % 8)) & 1)) s[i] = -INFINITY;
+    st.template raise<16, 32>(s, scale);
+    st.weigh(s, scale);
+    const bf16x8 p[2] = {weights8(s), weights8(s + 8)};
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int dt = 0; dt < ND; ++dt) st.o[dt] = mfma(__builtin_bit_cast(bf16x8, bf16_values(sb, dt, t)), p[t], st.o[dt]);
+    if (any_odd)
+      for (int t = 0; t < 32; ++t) {
+        float w = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) w = (t & 7) + 8 * (t >> 4) == i ? (float)p[i / 8][i % 8] : w;
+        odd(t, __shfl(w, 32 * ((t >> 3) & 1) + lj));
+      }
+  }
+
+  __device__ __forceinline__ float sum() const { return st.l + __shfl_xor(st.l, 32); }
+  template <typename F>
+  __device__ __forceinline__ void each4(F f) {
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        f(32 * dt + 8 * k + 4 * lh, f32x4{st.o[dt][4 * k], st.o[dt][4 * k + 1], st.o[dt][4 * k + 2], st.o[dt][4 * k + 3]});
+  }
+  template <typename F>
+  __device__ __forceinline__ void add4(F f) {
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) st.o[dt][i] = f(32 * dt + 8 * (i / 4) + 4 * lh + i % 4, st.o[dt][i]);
+  }
+};
 
 // Nodes 32 u .. of n into the LDS image of a bf16 unit, by the whole workgroup.  Values that
 // are not finite become 0 there (0 * NaN would carry a hidden node's values into every row);
 // returns whether this lane met one.
-template <int HD, int W>
+template <int HD, int W, int PAD>
 __device__ __forceinline__ bool stage_nodes(const TreeParams& p, u32x4* sb, int b, int g, int u, int n, int tid) {
-  using L = Unit<HD, false>;
+  using L = Unit<HD, false, PAD>;
   constexpr int C = HD / 8;
   const bf16* kb = (const bf16*)p.k.data + (int64_t)b * p.nodes * p.k.row + g * p.k.head;
   const bf16* vb = (const bf16*)p.v.data + (int64_t)b * p.nodes * p.v.row + g * p.v.head;
@@ -288,28 +520,6 @@ __device__ __forceinline__ bool stage_nodes(const TreeParams& p, u32x4* sb, int 
     }
   }
   return odd;
-}
-
-// The values of nodes 32 u .. that are not finite, added to the rows that see them with weight w
-// (row li's of nodes 8 la ..).
-template <int HD>
-__device__ __forceinline__ void add_odd_values(const TreeParams& p, Rows<HD>& st, bf16x8 weights, int b, int g, int u,
-                                               int n, int li, int la) {
-  const bf16* vb = (const bf16*)p.v.data + (int64_t)b * p.nodes * p.v.row + g * p.v.head;
-  for (int t = 0; t < 32 && 32 * u + t < n; ++t) {
-    float w = (float)weights[0];
-#pragma unroll
-    for (int e = 1; e < 8; ++e) w = (t & 7) == e ? (float)weights[e] : w;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const float wr = __shfl(w, 16 * (t >> 3) + 4 * la + r);
-#pragma unroll
-      for (int nt = 0; nt < HD / 16; ++nt) {
-        const float x = to_f32(vb[(int64_t)(32 * u + t) * p.v.row + 16 * nt + li]);
-        if (wr != 0.f && !(fabsf(x) <= 3.389531389e38f)) st.o[nt][r] = fmaf(wr, x, st.o[nt][r]);
-      }
-    }
-  }
 }
 
 // The (sequence, split) of work item `item`: first every split that is not its sequence's last,
@@ -353,9 +563,8 @@ __device__ __forceinline__ bool find_item(const TreeParams& p, int item, int lan
 }
 
 // Partial results: each tile of 16 rows in the order in which a wave holds it, four values (16 bytes) a
-// lane and side by side: o_part[tile of the split][nt][lane].  bf16 and 8-bit: rows 4 la + r of dim
-// 16 nt + li; fp32: dims 16 nt + 4 la + r of row li.  So both kernels move
-// whole lines.
+// lane and side by side: o_part[tile of the split][nt][16 la + li] = dims 16 nt + 4 la .. + 3 of row li.
+// So both kernels move whole lines.
 __device__ __forceinline__ int64_t tile_of(const TreeParams& p, int b, int g, int s, int row0) {
   return ((((int64_t)b * p.st.n_kv + g) * p.max_splits + s) * p.r_alloc + row0) >> 4;
 }
@@ -364,25 +573,27 @@ __device__ __forceinline__ float lse_of(float m, float l) {
   return l > 0.f || l != l ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
 }
 
-// One workgroup of four waves per (group of four query tiles, KV head; split; sequence), a tile each.
+// One workgroup of four waves per (group of query rows, KV head; split; sequence), 16 or 32 rows a wave.
 // The split's units pass through three LDS stages, loaded two units ahead, a quarter by every
 // wave (a wave without rows too).  A sequence's last split takes the nodes as well, first, while its
 // first units arrive.  A sequence of one split is finished here, else its splits leave (m, l) and O
 // for tree_merge.
 constexpr int kWaves = 4;
 
-template <int HD, bool E8>
+template <int HD, bool E8, template <int, bool> class Wave>
 __global__ __launch_bounds__(64 * kWaves, 3) void tree_split(const TreeParams p) {
-  using L = Unit<HD, E8>;
-  constexpr int NT = HD / 16, NC = HD / 32, NSUB = L::NSUB, U = L::TOKENS, IPG = L::IPG, W = kWaves;
+  using WV = Wave<HD, E8>;
+  using L = Unit<HD, E8, WV::PAD>;
+  constexpr int NSUB = L::NSUB, U = L::TOKENS, IPG = L::IPG, W = kWaves;
   constexpr int NS = 3, D = 2;  // LDS stages, units ahead
   // A wave loads the keys and values of one run of every unit (8-bit: four runs), or its keys or values (two).
   constexpr int KIND = NSUB == W ? 2 : 1, LOADS = KIND * IPG + (E8 ? 1 : 0);
   static_assert(KIND * W == 2 * NSUB && D * LOADS < 64, "every run once, and the loads in flight");
+  static_assert(L::PIECES >= Unit<HD, false, WV::PAD>::PIECES, "a stage holds a unit of nodes");
   __shared__ u32x4 stage[NS][L::PIECES];
   __shared__ int blk_ids[2][kIdWin];
   __shared__ int odd_values[W];
-  const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, la = lane >> 4;
+  const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   __builtin_assume(wave >= 0 && wave < W);
   const int g = blockIdx.x % p.st.n_kv, qg = blockIdx.x / p.st.n_kv;
@@ -393,22 +604,14 @@ __global__ __launch_bounds__(64 * kWaves, 3) void tree_split(const TreeParams p)
   const int n = count_of(p, b), rows = n * p.group;
   const int len = clamp_len(p.seq_lens, b, p.max_seq_len);
   const int t0 = s * p.split_len, t1 = min(len, t0 + p.split_len);
-  if ((s > 0 && t0 >= len) || qg * W * 16 >= rows) return;
+  if ((s > 0 && t0 >= len) || qg * W * WV::ROWS >= rows) return;
   const bool whole = len <= p.split_len, last = t1 == len;
-  const int row0 = (qg * W + wave) * 16;
+  const int row0 = (qg * W + wave) * WV::ROWS;
   const bool active = row0 < rows;
 
-  Rows<HD> st;
-  const int row = min(row0 + li, rows - 1), node = row / p.group, head = g * p.group + row % p.group;
-  {
-    const bf16* q = (const bf16*)p.q.data + ((int64_t)b * p.nodes + node) * p.q.row + (int64_t)head * p.q.head;
-#pragma unroll
-    for (int c = 0; c < NC; ++c) st.q[c] = __builtin_bit_cast(bf16x8, row8(q + 8 * (la * NC + c), p.q_vec));
-  }
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) st.o[nt] = f32x4{0.f, 0.f, 0.f, 0.f};
-  st.m = kNegBig;
-  st.l = 0.f;
+  WV wv(lane);
+  const int row = min(row0 + wv.row(), rows - 1), node = row / p.group, head = g * p.group + row % p.group;
+  wv.load_queries((const bf16*)p.q.data + ((int64_t)b * p.nodes + node) * p.q.row + (int64_t)head * p.q.head, p.q_vec);
 
   const StoreArg& c = p.st;
   constexpr int ESZ = E8 ? 1 : 2;
@@ -425,7 +628,7 @@ __global__ __launch_bounds__(64 * kWaves, 3) void tree_split(const TreeParams p)
     ids[j] = !bt_row ? b * c.mbps + lb0 + i : i < nlb ? bt_row[i] : 0;
   }
   if (last) {
-    const bool odd = stage_nodes<HD, W>(p, stage[D], b, g, 0, n, tid);
+    const bool odd = stage_nodes<HD, W, WV::PAD>(p, stage[D], b, g, 0, n, tid);
     const bool any = __any(odd);
     if (lane == 0) odd_values[wave] = any;
   }
@@ -498,7 +701,6 @@ __global__ __launch_bounds__(64 * kWaves, 3) void tree_split(const TreeParams p)
     ++next_u;
     look_ahead();
   };
-  bf16x8 weights;
   // nothing that the compiler counts stays in flight past this point
   wait_vmcnt<0>();
   lds_barrier();
@@ -511,26 +713,24 @@ __global__ __launch_bounds__(64 * kWaves, 3) void tree_split(const TreeParams p)
     for (int u = 0; 32 * u < n; ++u) {
       if (u > 0) {
         lds_barrier();
-        const bool odd = stage_nodes<HD, W>(p, stage[D], b, g, u, n, tid);
+        const bool odd = stage_nodes<HD, W, WV::PAD>(p, stage[D], b, g, u, n, tid);
         const bool any = __any(odd);
         if (lane == 0) odd_values[wave] = any;
         lds_barrier();
       }
       if (!active) continue;
-      const uint32_t seen = seen_word(p, b, node, u, n);
-      f32x4 sc[2];
-      Values<HD, false> x;
-      unit_scores<HD, false>(st, sc, stage[D], li, la);
-      read_values(x, stage[D], li, la);
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (!((seen >> (8 * la + i)) & 1)) sc[i / 4][i % 4] = -INFINITY;
-      raise_maximum(st, sc, p.scale_log2, la);
-      add_values<HD, false>(st, sc, x, weights, p.scale_log2);
       bool odd = false;
 #pragma unroll
       for (int w = 0; w < W; ++w) odd |= odd_values[w] != 0;
-      if (odd) add_odd_values<HD>(p, st, weights, b, g, u, n, li, la);
+      const bf16* vb = (const bf16*)p.v.data + (int64_t)b * p.nodes * p.v.row + g * p.v.head;
+      // the values that are not finite, kept out of the products, reach the rows that see them alone
+      wv.node_unit(stage[D], seen_word(p, b, node, u, n), p.scale_log2, odd, [&](int t, float w) {
+        if (32 * u + t >= n) return;
+        wv.add4([&](int d, float o) {
+          const float x = to_f32(vb[(int64_t)(32 * u + t) * p.v.row + d]);
+          return w != 0.f && !(fabsf(x) <= 3.389531389e38f) ? fmaf(w, x, o) : o;
+        });
+      });
     }
   int buf = 0;
   for (int u = 0; u < nunits; ++u) {
@@ -542,56 +742,40 @@ __global__ __launch_bounds__(64 * kWaves, 3) void tree_split(const TreeParams p)
     if (u + D <= lastu) issue(buf == 0 ? NS - 1 : buf - 1);
     const u32x4* sb = stage[buf];
     buf = buf == NS - 1 ? 0 : buf + 1;
-    if (!active) continue;
-    f32x4 sc[E8 ? 4 : 2];
-    Values<HD, E8> x;
-    unit_scores<HD, E8>(st, sc, sb, li, la);
-    // values are read once the scores' products are issued, into registers the keys held
-    __builtin_amdgcn_sched_barrier(0);
-    read_values(x, sb, li, la);
-    if (u == lastu) {
-      int limit = t1 - (t0 + U * u);
-      asm volatile("" : "+s"(limit));  // (keeps the masks a branch that whole units skip)
-      mask_tail(sc, limit, la);
-      clear_tail(x, limit, la);
-    }
-    raise_maximum(st, sc, p.scale_log2, la);
-    add_values<HD, E8>(st, sc, x, weights, p.scale_log2);
+    if (active) wv.cached_unit(sb, u == lastu, t1 - (t0 + U * u), p.scale_log2);
   }
 
   if (!active) return;
-  float l = st.l;
-  l += __shfl_xor(l, 16);
-  l += __shfl_xor(l, 32);
+  const float l = wv.sum();
+  const bool live = row0 + wv.row() < rows, first = lane < WV::ROWS;
   if (whole) {
-    if (p.lse && la == 0 && row0 + li < rows) p.lse[((int64_t)b * p.nodes + node) * (p.st.n_kv * p.group) + head] = lse_of(st.m, l);
+    if (!live) return;
+    if (p.lse && first) p.lse[((int64_t)b * p.nodes + node) * (p.st.n_kv * p.group) + head] = lse_of(wv.st.m, l);
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    bf16* o = (bf16*)p.out.data + ((int64_t)b * p.nodes + node) * p.out.row + (int64_t)head * p.out.head;
+    wv.each4([&](int d, f32x4 x) {
+      const bf16x4 y{(bf16)(x[0] * inv), (bf16)(x[1] * inv), (bf16)(x[2] * inv), (bf16)(x[3] * inv)};
+      if (p.o_vec) *reinterpret_cast<bf16x4*>(o + d) = y;
+      else
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const float lr = __shfl(l, 4 * la + r);
-      const float inv = lr == 0.f ? 0.f : 1.0f / lr;
-      const int orow = row0 + 4 * la + r;
-      if (orow >= rows) continue;
-      bf16* o = (bf16*)p.out.data + ((int64_t)b * p.nodes + orow / p.group) * p.out.row +
-                (int64_t)(g * p.group + orow % p.group) * p.out.head;
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) o[16 * nt + li] = (bf16)(st.o[nt][r] * inv);
-    }
+        for (int r = 0; r < 4; ++r) o[d + r] = y[r];
+    });
   } else {
-    const int64_t tile = tile_of(p, b, g, s, row0);
-    if (la == 0) p.ml_part[16 * tile + li] = make_float2(st.m, l);
-    if (row0 + 4 * la < rows)
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) ((f32x4*)p.o_part)[(tile * NT + nt) * 64 + lane] = st.o[nt];
+    const int64_t tile = tile_of(p, b, g, s, row0 + (wv.row() & ~15));
+    const int li = wv.row() & 15;
+    if (first) p.ml_part[16 * tile + li] = make_float2(wv.st.m, l);
+    if (live)
+      wv.each4([&](int d, f32x4 x) { ((f32x4*)p.o_part)[(tile * (HD / 16) + d / 16) * 64 + d % 16 / 4 * 16 + li] = x; });
   }
 }
 
 // Joins the splits of the sequences that have several: one workgroup per tile, every split's O
 // weighted by 2^(m - the largest m).  The 16 rows' weights of up to 32 splits at a time are found by
 // all threads and shared through LDS.
-template <int HD, typename T, bool F32>
+template <int HD, typename T>
 __global__ __launch_bounds__(256) void tree_merge(const TreeParams p) {
   constexpr int PER = HD / 64, CH = 32;
-  __shared__ __align__(16) float wsh[CH][16];
+  __shared__ float wsh[CH][16];
   __shared__ float red[16][17];
   const int tid = threadIdx.x, lane = tid & 63, li = lane & 15, la = lane >> 4;
   const int row0 = 16 * blockIdx.x, g = blockIdx.y, b = blockIdx.z;
@@ -606,7 +790,7 @@ __global__ __launch_bounds__(256) void tree_merge(const TreeParams p) {
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < 16; ++i) m = fmaxf(m, red[r][i]);
-  const bool mine = F32 ? row0 + li < rows : row0 + 4 * la < rows;  // whether the lane's values hold a row
+  const bool mine = row0 + li < rows;
   const f32x4* o = (const f32x4*)p.o_part + tile_of(p, b, g, 0, row0) * (HD * 4) + tid;
   const int64_t o_split = (int64_t)p.r_alloc / 16 * (HD * 4);
   f32x4 acc[PER];
@@ -633,8 +817,7 @@ __global__ __launch_bounds__(256) void tree_merge(const TreeParams p) {
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
         const f32x4 x = o[(s0 + k) * o_split + 256 * i];
-        if (F32) acc[i] += x * wsh[k][li];
-        else acc[i] += x * *reinterpret_cast<const f32x4*>(&wsh[k][4 * la]);
+        acc[i] += x * wsh[k][li];
       }
   }
   __syncthreads();
@@ -652,21 +835,20 @@ __global__ __launch_bounds__(256) void tree_merge(const TreeParams p) {
   }
   __syncthreads();
   if (!mine) return;
+  const int row = row0 + li;
+  const float inv = red[li][16];
+  T* out = (T*)p.out.data + ((int64_t)b * p.nodes + row / p.group) * p.out.row + (int64_t)(g * p.group + row % p.group) * p.out.head;
 #pragma unroll
-  for (int e = 0; e < (F32 ? 1 : 4); ++e) {
-    const int rr = F32 ? li : 4 * la + e, row = row0 + rr;
-    if (row >= rows) continue;
-    T* out = (T*)p.out.data + ((int64_t)b * p.nodes + row / p.group) * p.out.row + (int64_t)(g * p.group + row % p.group) * p.out.head;
+  for (int i = 0; i < PER; ++i) {
+    const int d = ((256 * i + tid) >> 6) * 16 + 4 * la;
+    typedef T T4 __attribute__((ext_vector_type(4)));
+    T4 y;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int nt = (256 * i + tid) >> 6;
-      if (F32) {
+    for (int r = 0; r < 4; ++r) y[r] = from_f32<T>(acc[i][r] * inv);
+    if (p.o_vec) *reinterpret_cast<T4*>(out + d) = y;
+    else
 #pragma unroll
-        for (int d = 0; d < 4; ++d) out[16 * nt + 4 * la + d] = from_f32<T>(acc[i][d] * red[rr][16]);
-      } else {
-        out[16 * nt + li] = from_f32<T>(acc[i][e] * red[rr][16]);
-      }
-    }
+      for (int r = 0; r < 4; ++r) out[d + r] = y[r];
   }
 }
 
@@ -839,25 +1021,25 @@ hipError_t launch_tree(const TreeParams& p, int storage, int hd, hipStream_t s) 
     else hipLaunchKernelGGL((tree_split_f32<64>), grid, block, 0, s, p);
     e = hipGetLastError();
   } else {
-    if (p.split_len % 64 || p.r_alloc < rows || p.r_alloc != p.n_qgroups * 16 * kWaves) return hipErrorInvalidValue;
+    if (p.split_len % 64 || p.r_alloc < rows || p.r_alloc != p.n_qgroups * p.rows_per_wave * kWaves) return hipErrorInvalidValue;
     const dim3 grid(p.st.n_kv * p.n_qgroups, p.max_splits, p.st.batch), block(64 * kWaves);
-    if (storage == SP_E4M3) {
-      if (hd == 128) hipLaunchKernelGGL((tree_split<128, true>), grid, block, 0, s, p);
-      else hipLaunchKernelGGL((tree_split<64, true>), grid, block, 0, s, p);
-    } else {
-      if (hd == 128) hipLaunchKernelGGL((tree_split<128, false>), grid, block, 0, s, p);
-      else hipLaunchKernelGGL((tree_split<64, false>), grid, block, 0, s, p);
-    }
+    const bool e8 = storage == SP_E4M3;
+#define SP_TREE(HD_, E8_, ROWS_)                                                                   \
+  if (hd == HD_ && e8 == E8_ && p.rows_per_wave == ROWS_)                                          \
+    hipLaunchKernelGGL((tree_split<HD_, E8_, Wave##ROWS_>), grid, block, 0, s, p);
+    SP_TREE(128, false, 16) SP_TREE(128, false, 32) SP_TREE(128, true, 16) SP_TREE(128, true, 32)
+    SP_TREE(64, false, 16) SP_TREE(64, false, 32) SP_TREE(64, true, 16) SP_TREE(64, true, 32)
+#undef SP_TREE
     e = hipGetLastError();
   }
   if (e != hipSuccess || p.max_splits == 1) return e;
   const dim3 mgrid((rows + 15) / 16, p.st.n_kv, p.st.batch), block(256);
   if (storage == SP_F32) {
-    if (hd == 128) hipLaunchKernelGGL((tree_merge<128, float, true>), mgrid, block, 0, s, p);
-    else hipLaunchKernelGGL((tree_merge<64, float, true>), mgrid, block, 0, s, p);
+    if (hd == 128) hipLaunchKernelGGL((tree_merge<128, float>), mgrid, block, 0, s, p);
+    else hipLaunchKernelGGL((tree_merge<64, float>), mgrid, block, 0, s, p);
   } else {
-    if (hd == 128) hipLaunchKernelGGL((tree_merge<128, bf16, false>), mgrid, block, 0, s, p);
-    else hipLaunchKernelGGL((tree_merge<64, bf16, false>), mgrid, block, 0, s, p);
+    if (hd == 128) hipLaunchKernelGGL((tree_merge<128, bf16>), mgrid, block, 0, s, p);
+    else hipLaunchKernelGGL((tree_merge<64, bf16>), mgrid, block, 0, s, p);
   }
   return hipGetLastError();
 }

@@ -183,7 +183,7 @@ class PagedCache:
             _need(k_exponents is None and v_exponents is None, "exponents belong to float8 caches")
         self.c, self.c_dtype = st, st.dtype
         self.table = None if block_table is None else block_table.data_ptr()
-        self.capacity = min(self.max_blocks * block_size, (1 << 31) - 1)  # tokens of a sequence
+        self.capacity = min(self.max_blocks * block_size, 1 << 30)  # tokens of a sequence that attention reads
 
     @classmethod
     def allocate(cls, dtype, num_blocks, n_kv_heads, head_dim, block_size=16, block_table=None, batch=None, device="cuda"):

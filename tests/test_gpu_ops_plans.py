@@ -174,3 +174,50 @@ def test_random_rows_in_and_out_of_a_cache(dev, seed):
             assert torch.equal(got.cpu().double(), val * torch.exp2(byte.double() - 127)[..., None])
     else:
         assert torch.equal(k, x[:, :nkv].to(store).float()) and torch.equal(v, x[:, nkv:].to(store).float())
+
+
+@pytest.mark.parametrize("store", STORES)
+@pytest.mark.parametrize("hd,nodes,nq,nkv", [(128, 64, 8, 2), (128, 43, 12, 2), (64, 256, 3, 3), (64, 33, 32, 4), (128, 3, 64, 1)])
+@pytest.mark.parametrize("cut", [False, True])
+@pytest.mark.parametrize("much", [False, True])
+def test_many_query_rows(dev, store, hd, nodes, nq, nkv, cut, much):
+    """192 rows and more per KV head, whole groups and partly filled ones, sequences of one split and of several,
+    masks that leave rows empty, nodes that are not finite; planned for the lengths at hand (waves of 16 rows), and for
+    as many tokens as waves of 32 rows take."""
+    lens = (0, 1, 33, 47, 64, 1000, 2700) if cut else (700, 13)
+    c = Tree(dev, store, lens, nodes, nq, nkv, hd, 16, seed=66 + nodes)
+    batch, gen = len(lens), seeded(67)
+    bound = max(lens)
+    if much:
+        groups = -(-nodes * nq // nkv // 128)
+        bound = max(bound, 256 * -(-6 * 256 // (nkv * batch * groups)))
+        table = c.cache.block_table
+        table = torch.cat([table, table[:, -1:].expand(-1, -(-bound // 16) - table.shape[1])], 1).contiguous()
+        c.cache = ops.PagedCache(c.cache.k, c.cache.v, 16, table, c.cache.k_exponents, c.cache.v_exponents)
+    see = c.see & (torch.rand(c.see.shape, generator=gen) < 0.7)
+    see[:, :, nodes // 2] = False
+    x, calm = c.x.clone(), c.x.clone()
+    x[:, nodes // 2, nq:] = math.nan  # seen by nobody
+    calm[:, nodes // 2, nq:] = 0
+    counts = [int(n) for n in torch.randint(1, nodes + 1, (batch,), generator=gen)] if cut else [nodes] * batch
+    q, k, v = c.qkv(x)
+    out = torch.full(q.shape, 3.0, dtype=c.dtype, device=dev)
+    lse = torch.full(q.shape[:3], 3.0, device=dev)
+    ops.tree_attention(c.cache, c.seq_lens, q, k, v, mask=words_of(see).to(dev), out=out, lse=lse,
+                       counts=torch.tensor(counts, dtype=torch.int32, device=dev), max_seq_len=bound)
+    c.check(out, lse, see=see, counts=counts, x=calm)
+    for b, n in enumerate(counts):
+        assert torch.all(out[b, n:] == 3.0) and torch.all(lse[b, n:] == 3.0)
+    # infinite values reach the rows that see them, and those rows only
+    see[:, :, nodes // 2] = torch.rand((batch, nodes), generator=gen) < 0.5
+    x = c.x.clone()
+    x[:, nodes // 2, nq + nkv:] = math.inf
+    q, k, v = c.qkv(x)
+    got = ops.tree_attention(c.cache, c.seq_lens, q, k, v, mask=words_of(see).to(dev), max_seq_len=bound).cpu()
+    hit = see[:, :, nodes // 2].clone()
+    assert torch.all(got[hit].float() == math.inf)
+    see[:, :, nodes // 2] = False
+    rest = ops.tree_attention(c.cache, c.seq_lens, *c.qkv(), mask=words_of(see).to(dev), max_seq_len=bound).cpu()
+    # (to the tolerance, not to the bit: rows of a wave move their reference maximum together, so what one of them sees
+    # can change at which power of two another's weights are rounded)
+    c.check(torch.where(hit[:, :, None, None], rest, got), see=see)

@@ -255,3 +255,17 @@ def test_the_oracle_rounds_as_e4m3():
     assert float(v.abs().max()) <= 448 and bool((v[2:].abs().amax(-1) > 223).all())
     w, _ = oracle.quantise(torch.tensor([[math.inf, -1.0, math.nan, 2.0]]))
     assert torch.isnan(w[0, [0, 2]]).all() and w[0, [1, 3]].tolist() == [-128.0, 256.0]
+
+
+def test_the_longest_context():
+    lib = binding.load()
+    cfg = binding.sp_tree_config(n_q_heads=8, n_kv_heads=2, head_dim=128, dtype=1, kv_dtype=1, max_nodes=8, max_batch=1,
+                                 max_seq_len=1 << 30)
+    assert lib.sp_probe_tree_workspace_bytes(ctypes.byref(cfg)) > 0
+    cfg.max_seq_len += 1
+    assert lib.sp_probe_tree_workspace_bytes(ctypes.byref(cfg)) == 0
+    t = binding.sp_tree(n_nodes=4, q=rows(8), k=rows(2), v=rows(2), out=rows(8))
+    assert lib.sp_probe_tree_attention(ctypes.byref(cfg), ctypes.byref(store()), P, P, ctypes.byref(t), P, 1 << 40, None) == UNSUPPORTED
+    # a table whose rows reach further gives attention that many tokens at most
+    table = torch.zeros((1, 1 << 16), dtype=torch.int32)
+    assert ops.PagedCache.allocate(torch.bfloat16, 1, 1, 64, 1 << 15, table, device="cpu").capacity == 1 << 30
