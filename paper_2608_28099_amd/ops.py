@@ -74,11 +74,15 @@ def _rows(t, name, head_dim, dtype, device, n=None):
         raise ValueError(f"{name} must be {dtype} on {device}")
     if stride[-1] != 1:
         raise ValueError(f"{name}: the values of a head must lie side by side")
-    if len(shape) == 4 and shape[0] != 1 and stride[0] != shape[1] * stride[1]:
-        raise ValueError(f"{name}: rows must be evenly spaced")
+    row = stride[-3]
+    if len(shape) == 4 and shape[0] != 1:
+        if shape[1] == 1:
+            row = stride[0]  # (the stride of a dimension of one means nothing)
+        elif stride[0] != shape[1] * row:
+            raise ValueError(f"{name}: rows must be evenly spaced")
     if n is not None and shape[0] != n:
         raise ValueError(f"{name} must have {n} rows")
-    return binding.sp_rows(t.data_ptr(), stride[-3], stride[-2], shape[-2], 0)
+    return binding.sp_rows(t.data_ptr(), row, stride[-2], shape[-2], 0)
 
 
 def _ids(t, name, n, device):

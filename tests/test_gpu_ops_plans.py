@@ -221,3 +221,12 @@ def test_many_query_rows(dev, store, hd, nodes, nq, nkv, cut, much):
     # (to the tolerance, not to the bit: rows of a wave move their reference maximum together, so what one of them sees
     # can change at which power of two another's weights are rounded)
     c.check(torch.where(hit[:, :, None, None], rest, got), see=see)
+
+
+@pytest.mark.parametrize("store", STORES)
+def test_single_nodes_of_packed_projections(dev, store):
+    c = Tree(dev, store, (300, 0, 17), 1, 8, 2, 128, 16, seed=68)
+    ref = ops.tree_attention(c.cache, c.seq_lens, *c.qkv(), max_seq_len=300)
+    packed = c.x[:, 0].to(dev)  # [batch, heads, hd]
+    q, k, v = (x.unsqueeze(1) for x in packed.split([8, 2, 2], 1))
+    assert torch.equal(ops.tree_attention(c.cache, c.seq_lens, q, k, v, max_seq_len=300), ref)

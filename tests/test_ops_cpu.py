@@ -269,3 +269,16 @@ def test_the_longest_context():
     # a table whose rows reach further gives attention that many tokens at most
     table = torch.zeros((1, 1 << 16), dtype=torch.int32)
     assert ops.PagedCache.allocate(torch.bfloat16, 1, 1, 64, 1 << 15, table, device="cpu").capacity == 1 << 30
+
+
+def test_rows_of_single_nodes():
+    """[batch, 1, heads, hd] taken from packed projections: the rows' step is the batch's stride."""
+    packed = torch.zeros(3, 12, 64)
+    r = ops._rows(packed[:, :8].unsqueeze(1), "q", 64, torch.float32, packed.device)
+    assert (r.stride_row, r.stride_head, r.n_heads) == (12 * 64, 64, 8)
+    r = ops._rows(packed.view(3, 1, 12, 64)[:, :, 8:], "k", 64, torch.float32, packed.device)
+    assert (r.stride_row, r.n_heads) == (12 * 64, 4)
+    r = ops._rows(packed[None, :, :8], "q", 64, torch.float32, packed.device)  # one sequence of three nodes
+    assert (r.stride_row, r.n_heads) == (12 * 64, 8)
+    with pytest.raises(ValueError):
+        ops._rows(torch.zeros(2, 4, 12, 64)[:, :3], "q", 64, torch.float32, packed.device)
