@@ -334,14 +334,16 @@ SP_API int sp_probe_cache_write(const sp_kv_store* store, const int32_t* block_t
                                 int32_t n_src, const sp_rows* k, const sp_rows* v, const sp_rotary* rot,
                                 void* stream) {
   CacheParams p{};
-  int st = cache_params(store, block_table, dtype, n_rows, seq_ids, positions, k, v, &p);
+  // no source row: every row is skipped, k and v need not exist
+  const bool none = n_src == 0;
+  int st = cache_params(store, block_table, dtype, n_rows, seq_ids, positions, none ? nullptr : k, none ? nullptr : v, &p);
   if (st != SP_OK) return st;
   if (rot) {
     if ((st = check_rotary(rot)) != SP_OK) return st;
     if (rot->head_dim != store->head_dim) return SP_ERR_INVALID_ARG;
   }
   if (n_src < 0) return SP_ERR_INVALID_ARG;
-  if (n_rows == 0 || n_src == 0) return SP_OK;  // no source row: every row is skipped
+  if (n_rows == 0 || none) return SP_OK;
   if (!k || !v || (src_rows && !aligned(src_rows, 4))) return SP_ERR_INVALID_ARG;
   int cus = 0;
   if ((st = current_device(&cus)) != SP_OK) return st;

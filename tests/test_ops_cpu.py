@@ -282,3 +282,11 @@ def test_rows_of_single_nodes():
     assert (r.stride_row, r.n_heads) == (12 * 64, 8)
     with pytest.raises(ValueError):
         ops._rows(torch.zeros(2, 4, 12, 64)[:, :3], "q", 64, torch.float32, packed.device)
+
+
+def test_rows_without_a_source():
+    lib = binding.load()
+    nothing = rows(2, None)
+    for n_src, want in ((0, 0), (1, BAD)):
+        assert lib.sp_probe_cache_write(ctypes.byref(store()), P, binding.SP_BF16, 3, P, P, P, n_src, ctypes.byref(nothing),
+                                        ctypes.byref(nothing), None, None) == want
