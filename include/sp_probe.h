@@ -372,7 +372,8 @@ int sp_probe_measure_mfma(int32_t iters, void* sink, float* tflops, void* stream
  * Operators on the head's paged cache: what a server does to it beside the
  * classification forward.  They take no handle, allocate nothing, enqueue one
  * or two kernels on `stream` and can be captured into a HIP graph; every
- * check that the host can make runs before anything is enqueued.
+ * check that the host can make runs before anything is enqueued.  A call takes
+ * less than 2^26 rows (n_rows); more: SP_ERR_UNSUPPORTED.
  * ---------------------------------------------------------------------- */
 
 /* 8-bit storage of a cache (sp_kv_store.dtype, beside SP_F32 and SP_BF16): E4M3

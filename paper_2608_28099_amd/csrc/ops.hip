@@ -21,6 +21,9 @@ bool is_pow2(int64_t x) { return x > 0 && (x & (x - 1)) == 0; }
 int ilog2(int64_t x) { int r = 0; while ((int64_t(1) << r) < x) ++r; return r; }
 int size_of(int dtype) { return dtype == SP_F32 ? 4 : dtype == SP_BF16 ? 2 : 1; }
 
+// Rows of a call: a launch has less than 2^32 threads along x, and a rotation takes 64 per row.
+constexpr int kMaxRows = (1 << 26) - 1;
+
 // The current device: whether the kernels run on it, and its compute units (asked once).
 constexpr int kMaxDevices = 64;
 struct DeviceInfo {
@@ -273,6 +276,7 @@ SP_API int sp_probe_rotary(const sp_rotary* rot, int32_t dtype, int32_t transpos
   if (n_rows < 0 || !q || !q_out || (k == nullptr) != (k_out == nullptr)) return SP_ERR_INVALID_ARG;
   if (q->n_heads < 1 || (k && k->n_heads < 1)) return SP_ERR_INVALID_ARG;
   if (q->n_heads > 4096 || (k && k->n_heads > 4096)) return SP_ERR_UNSUPPORTED;
+  if (n_rows > kMaxRows) return SP_ERR_UNSUPPORTED;
   if (n_rows == 0) return SP_OK;
   if (!positions || !aligned(positions, 4)) return SP_ERR_INVALID_ARG;
   const int esz = size_of(dtype);
@@ -307,6 +311,7 @@ int cache_params(const sp_kv_store* store, const int32_t* block_table, int32_t d
   if (st != SP_OK) return st;
   if (dtype != SP_F32 && dtype != SP_BF16) return SP_ERR_INVALID_ARG;
   if (n_rows < 0) return SP_ERR_INVALID_ARG;
+  if (n_rows > kMaxRows) return SP_ERR_UNSUPPORTED;
   if (n_rows == 0) return SP_OK;
   if (!seq_ids || !positions || !aligned(seq_ids, 4) || !aligned(positions, 4)) return SP_ERR_INVALID_ARG;
   bool k_vec = true, v_vec = true;

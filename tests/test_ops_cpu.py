@@ -290,3 +290,13 @@ def test_rows_without_a_source():
     for n_src, want in ((0, 0), (1, BAD)):
         assert lib.sp_probe_cache_write(ctypes.byref(store()), P, binding.SP_BF16, 3, P, P, P, n_src, ctypes.byref(nothing),
                                         ctypes.byref(nothing), None, None) == want
+
+
+def test_the_most_rows():
+    lib = binding.load()
+    rot = ops.make_rotary(128)
+    q, k = rows(2), rows(2)
+    n = 1 << 26
+    assert lib.sp_probe_rotary(rot, binding.SP_BF16, 0, n, P, q, q, None, None, None) == UNSUPPORTED
+    assert lib.sp_probe_cache_write(store(), P, binding.SP_BF16, n, P, P, None, n, k, k, None, None) == UNSUPPORTED
+    assert lib.sp_probe_cache_read(store(), P, binding.SP_BF16, n, P, P, k, k, None) == UNSUPPORTED
