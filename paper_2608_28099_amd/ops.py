@@ -9,8 +9,11 @@
 Thin marshalling over the C functions of include/sp_probe.h (sp_probe_rotary,
 sp_probe_cache_write, sp_probe_cache_read, sp_probe_tree_attention), which document the
 operations.  Calls go to the given stream (a raw handle; default: the current
-stream of the tensors' device) and return without waiting.  Wrong types, shapes and
+stream of the tensors' device) and return without waiting; a given stream's order against the
+streams that made the inputs and read the results is the caller's to keep.  Wrong types, shapes and
 devices raise ValueError here, what the library refuses raises binding.ProbeError.
+Results carry no autograd graph: a rotation's gradient is its transpose, and the other operators are
+for serving.
 """
 from __future__ import annotations
 
@@ -51,13 +54,16 @@ def _elsewhere(device):
     return device.index is not None and device.index != _current_device()
 
 
-def _hold(stream, device, *tensors):
-    """Memory that a call made lives until the given stream is past it."""
-    if stream is not None:
-        s = torch.cuda.ExternalStream(stream, device=device)
-        for t in tensors:
-            if t is not None:
-                t.record_stream(s)
+def _empty(shape, dtype, device, stream):
+    """Memory for a call: of the given stream's pool, so that nothing enqueued elsewhere still uses it, and
+    once freed not handed out again before the current stream, which may read it, is past that."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    now = torch.cuda.current_stream(device)
+    with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device)):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(now)
+    return t
 
 
 def _check(status, what):
@@ -124,16 +130,15 @@ def rotary(rot, positions, q, k=None, out=None, k_out=None, transpose=False, str
     if _elsewhere(dev):
         with torch.cuda.device(dev):
             return rotary(rot, positions, q, k, out, k_out, transpose, stream)
-    made = made_k = None
     if out is None:
-        out = made = torch.empty_like(q, memory_format=torch.contiguous_format)
+        out = _empty(q.shape, dtype, dev, stream)
     elif out.shape != q.shape:
         raise ValueError("out must have q's shape")
     qr, outr = _rows(q, "q", hd, dtype, dev, n), _rows(out, "out", hd, dtype, dev, n)
     kr = k_outr = None
     if k is not None:
         if k_out is None:
-            k_out = made_k = torch.empty_like(k, memory_format=torch.contiguous_format)
+            k_out = _empty(k.shape, k.dtype, dev, stream)
         elif k_out.shape != k.shape:
             raise ValueError("k_out must have k's shape")
         kr, k_outr = _rows(k, "k", hd, dtype, dev, n), _rows(k_out, "k_out", hd, dtype, dev, n)
@@ -141,7 +146,6 @@ def rotary(rot, positions, q, k=None, out=None, k_out=None, transpose=False, str
                                           _ids(positions, "positions", n, dev), qr, outr, kr, k_outr,
                                           _current_stream(_current_device()) if stream is None else stream),
            "sp_probe_rotary")
-    _hold(stream, dev, made, made_k)
     return out if k is None else (out, k_out)
 
 
@@ -235,10 +239,9 @@ def cache_read(cache: PagedCache, seq_ids, positions, dtype=torch.bfloat16, k=No
     if _elsewhere(dev):
         with torch.cuda.device(dev):
             return cache_read(cache, seq_ids, positions, dtype, k, v, stream)
-    made_k = made_v = None
     if k is None and v is None:
-        k = made_k = torch.empty((n, cache.n_kv_heads, hd), dtype=dtype, device=dev)
-        v = made_v = torch.empty_like(k)
+        k = _empty((n, cache.n_kv_heads, hd), dtype, dev, stream)
+        v = _empty((n, cache.n_kv_heads, hd), dtype, dev, stream)
     else:
         dtype = k.dtype if k is not None else v.dtype
     if dtype not in _ROW_TYPES:
@@ -248,7 +251,6 @@ def cache_read(cache: PagedCache, seq_ids, positions, dtype=torch.bfloat16, k=No
         _ids(positions, "positions", n, dev), None if k is None else _rows(k, "k", hd, dtype, dev, n),
         None if v is None else _rows(v, "v", hd, dtype, dev, n),
         _current_stream(_current_device()) if stream is None else stream), "sp_probe_cache_read")
-    _hold(stream, dev, made_k, made_v)
     return k, v
 
 
@@ -306,9 +308,8 @@ def tree_attention(cache: PagedCache, seq_lens, q, k, v, mask=None, counts=None,
         with torch.cuda.device(dev):
             return tree_attention(cache, seq_lens, q, k, v, mask, counts, max_seq_len, scale or None, out, lse, workspace,
                                   stream)
-    made = made_ws = None
     if out is None:
-        out = made = torch.empty_like(q, memory_format=torch.contiguous_format)
+        out = _empty(shape, dtype, dev, stream)
     elif out.shape != shape:
         raise ValueError("out must have q's shape")
     tree = binding.sp_tree(nodes, 0, None if counts is None else _ids(counts, "counts", batch, dev), None, 0,
@@ -328,14 +329,13 @@ def tree_attention(cache: PagedCache, seq_lens, q, k, v, mask=None, counts=None,
     cfg = _tree_config(cache, nq, dtype, nodes, batch or 1, max_seq_len, scale)
     lib = binding.load()
     if workspace is None:
-        workspace = made_ws = torch.empty(max(lib.sp_probe_tree_workspace_bytes(cfg), 16), dtype=torch.uint8, device=dev)
+        workspace = _empty(max(lib.sp_probe_tree_workspace_bytes(cfg), 16), torch.uint8, dev, stream)
     elif workspace.dtype != torch.uint8 or workspace.device != dev or not workspace.is_contiguous():
         raise ValueError(f"workspace must be contiguous uint8 on {dev}")
     _check(lib.sp_probe_tree_attention(cfg, cache.c, _ids(seq_lens, "seq_lens", batch, dev), cache.table, tree,
                                        workspace.data_ptr(), workspace.numel(),
                                        _current_stream(_current_device()) if stream is None else stream),
            "sp_probe_tree_attention")
-    _hold(stream, dev, made, made_ws)
     return out
 
 

@@ -230,3 +230,26 @@ def test_single_nodes_of_packed_projections(dev, store):
     packed = c.x[:, 0].to(dev)  # [batch, heads, hd]
     q, k, v = (x.unsqueeze(1) for x in packed.split([8, 2, 2], 1))
     assert torch.equal(ops.tree_attention(c.cache, c.seq_lens, q, k, v, max_seq_len=300), ref)
+
+
+def test_results_on_a_given_stream_use_that_streams_memory(dev):
+    """Memory that the current stream still reads (freed, but its work is pending) is not written by a call on
+    another stream; results outlive the call's own references."""
+    side = torch.cuda.Stream()
+    rot = ops.make_rotary(128)
+    q = torch.randn(4096, 8, 128, device=dev)
+    pos = torch.arange(4096, dtype=torch.int32, device=dev)
+    ref = ops.rotary(rot, pos, q)
+    torch.cuda.synchronize()
+    a = torch.full(q.shape, 2.0, device=dev)
+    b = torch.randn(4096, 4096, device=dev)
+    torch.cuda.synchronize()
+    for _ in range(20):  # some milliseconds before the sum below
+        b = torch.mm(b, b).clamp_(-1, 1)
+    total = a.sum(dtype=torch.float64)
+    at = a.data_ptr()
+    del a
+    y = ops.rotary(rot, pos, q, stream=side.cuda_stream)
+    assert y.data_ptr() != at
+    torch.cuda.synchronize()
+    assert float(total) == 2.0 * q.numel() and torch.equal(y, ref)
