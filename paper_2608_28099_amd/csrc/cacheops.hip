@@ -117,14 +117,15 @@ __device__ __forceinline__ PairOf pair_of(int d, int rotary_dim, int layout) {
 }
 
 // ---------------------------------------------------------------- rotary
-// One workgroup per R rows: their cosines and sines once into LDS (fp64 angles), then each thread
-// takes the same piece of every row, so that R rows' loads are under way together.  A pair
+// y0 = x0 cos a - x1 sin a, y1 = x1 cos a + x0 sin a for every pair: every value read and written once, so
+// bound by memory.  One workgroup per R rows: their cosines and sines once into LDS (fp64 angles), then each
+// thread takes the same piece of every row, so that R rows' loads are under way together.  A pair
 // is read and written by one lane, so the output may be the input.  Pieces (V values, 16
 // bytes, where every head is aligned so): of interleaved heads V values of a head; of half
 // heads V pairs, or V values that stay.  Else single pairs and values (kScalar).
-// 16384 rows of 48 heads (half of each rotated, bf16, 403 MB): see launch_rotary.
+// 16384 rows of 48 heads (half of each rotated, bf16, 403 MB): 80 us, 5.0 TB/s, where a large copy moves
+// 4.8; 128 rows of 40: 3.8 us.  (Which R and pieces: rotary_typed.)
 enum RotaryMode { kScalar, kHalf, kInterleaved };
-constexpr int kRotaryRows = 4;
 
 template <typename T, int MODE, int R>
 __global__ __launch_bounds__(256) void rotary_rows(const RotaryParams p) {
@@ -260,6 +261,8 @@ __device__ __forceinline__ void pack(const float (&x)[16], Stored<TS>& out, int&
 // a tile fill an aligned group of 16 bytes' worth of slots (a "group": 4, 8 or 16 rows that
 // follow one another), each dim of it is one 16-byte store; what is left, at a run's
 // ends or with scattered rows, is stored value by value.
+// 49152 rows of 8 heads (bf16 rows, head dim 128): 8-bit 61 us (302 MB, 4.9 TB/s), with a rotation 87 (the angles, and
+// four heads in turn); bf16 94 us (403 MB, 4.3 TB/s), rotated 97.  128 rows: 4.4 to 4.9 us, rotated 8.4 to 9.
 constexpr int kTile = 64;
 
 struct TilePlan {
@@ -450,7 +453,8 @@ __global__ __launch_bounds__(256) void cache_write(const CacheParams p, const sp
 
 // ---------------------------------------------------------------- read
 // The same tiles the other way, a workgroup per KV head for the keys and one for the values: values
-// through LDS, by groups where the tokens make them.
+// through LDS, by groups where the tokens make them.  49152 rows of 8 heads to bf16 (head dim 128): from 8-bit 79 us
+// (302 MB, 3.8 TB/s: 1-byte LDS writes and reads of the values' transposition), from bf16 82 (4.9 TB/s).
 template <typename TS>
 __device__ __forceinline__ float value_of(TS x) {
   if constexpr (sizeof(TS) == 1) return __builtin_amdgcn_cvt_f32_fp8((int)x.bits, 0);
@@ -540,34 +544,44 @@ hipError_t read_typed(const CacheParams& p, int hd, dim3 grid, hipStream_t s) {
   return hipGetLastError();
 }
 
-// KV heads of a workgroup of keys: one, or with a rotation as many as leave four workgroups per
-// compute unit (their angles are found once).
+// KV heads of a workgroup of keys: one, or with a rotation up to four that leave a workgroup per compute
+// unit (their angles are found once, but their rows pass one after the other).  Rows of 8 heads, bf16 and
+// 8-bit, in us with 1 / 2 / 4 / 8 heads a workgroup: 2048 rows 10.7 / 11.2 / 13.0 / 16.9 and 10.9 / 12.1 / 15.2 / 21.6; 8192 rows
+// 27.2 / 19.7 / 19.9 / 24.8 and 26.0 / 22.4 / 20.1 / 27.3; 49152 rows 124 / 105 / 98 / 104 and 119 / 96 / 87 / 86.
 int heads_per_wg(const CacheParams& p, int n_cus) {
   if (!p.rot) return 1;
   const int64_t tiles = (p.n_rows + kTile - 1) / kTile;
-  int hpw = p.st.n_kv;
-  while (hpw > 1 && tiles * ((p.st.n_kv + hpw - 1) / hpw) < 4 * (int64_t)n_cus) hpw = (hpw + 1) / 2;
+  int hpw = p.st.n_kv < 4 ? p.st.n_kv : 4;
+  while (hpw > 1 && tiles * ((p.st.n_kv + hpw - 1) / hpw) < n_cus) hpw = (hpw + 1) / 2;
   return hpw;
 }
 
-template <typename T, int R>
-hipError_t rotary_typed(const RotaryParams& p, hipStream_t s) {
+// 16-byte pieces where alignment allows them (bf16, 48 heads, half of each turned: 128 rows 4.5 us, in
+// single values 11.6; 16384 rows 80 and 165).  One row a workgroup, but four of interleaved
+// heads where that leaves four workgroups per compute unit (40 heads, 16384 rows: 75 us with one, 66 with four; 1024 rows 6.4 and
+// 7.8; half heads, 16384 rows: 61 and 65).
+template <typename T>
+hipError_t rotary_typed(const RotaryParams& p, int n_cus, hipStream_t s) {
   constexpr int V = 16 / sizeof(T);
-  const dim3 grid((p.n_rows + R - 1) / R), block(256);
-  if (p.vec && p.rot.layout == SP_ROTARY_INTERLEAVED) hipLaunchKernelGGL((rotary_rows<T, kInterleaved, R>), grid, block, 0, s, p);
-  else if (p.vec && p.rot.rotary_dim % (2 * V) == 0) hipLaunchKernelGGL((rotary_rows<T, kHalf, R>), grid, block, 0, s, p);
-  else hipLaunchKernelGGL((rotary_rows<T, kScalar, R>), grid, block, 0, s, p);
+  const dim3 grid(p.n_rows), block(256);
+  if (p.vec && p.rot.layout == SP_ROTARY_INTERLEAVED) {
+    constexpr int R = 4;
+    if (p.n_rows >= 4 * R * n_cus)
+      hipLaunchKernelGGL((rotary_rows<T, kInterleaved, R>), dim3((p.n_rows + R - 1) / R), block, 0, s, p);
+    else hipLaunchKernelGGL((rotary_rows<T, kInterleaved, 1>), grid, block, 0, s, p);
+  } else if (p.vec && p.rot.rotary_dim % (2 * V) == 0) {
+    hipLaunchKernelGGL((rotary_rows<T, kHalf, 1>), grid, block, 0, s, p);
+  } else {
+    hipLaunchKernelGGL((rotary_rows<T, kScalar, 1>), grid, block, 0, s, p);
+  }
   return hipGetLastError();
 }
 
 }  // namespace
 
-// Four rows a workgroup where that leaves four workgroups per compute unit, else one.
 hipError_t launch_rotary(const RotaryParams& p, int bf16_rows, int n_cus, hipStream_t s) {
   if (p.n_rows <= 0) return hipSuccess;
-  if (p.n_rows >= 4 * kRotaryRows * n_cus)
-    return bf16_rows ? rotary_typed<bf16, kRotaryRows>(p, s) : rotary_typed<float, kRotaryRows>(p, s);
-  return bf16_rows ? rotary_typed<bf16, 1>(p, s) : rotary_typed<float, 1>(p, s);
+  return bf16_rows ? rotary_typed<bf16>(p, n_cus, s) : rotary_typed<float>(p, n_cus, s);
 }
 
 hipError_t launch_cache_write(const CacheParams& p0, int storage, int bf16_rows, int hd, int n_cus, hipStream_t s) {
