@@ -461,44 +461,45 @@ __device__ __forceinline__ float value_of(TS x) {
   else return to_f32(x);
 }
 
+template <typename T>
+__device__ __forceinline__ void store8(T* p, bool vec, const float (&x)[8]) {
+  if (vec) {
+    if constexpr (sizeof(T) == 2) {
+      bf16x8 w;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i] = (bf16)x[i];
+      *reinterpret_cast<u32x4*>(p) = __builtin_bit_cast(u32x4, w);
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) *reinterpret_cast<f32x4*>(p + 4 * h) = f32x4{x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]};
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) p[i] = from_f32<T>(x[i]);
+  }
+}
+
 template <typename TS, typename TI, int HD>
 __global__ __launch_bounds__(256) void cache_read(const CacheParams p) {
   constexpr int LR = HD / 16, RP = 256 / LR, X = 16 / sizeof(TS);
-  constexpr int VP = kTile + 4 / sizeof(TS);
+  constexpr int Q = 4 / sizeof(TS);  // values of a word
+  constexpr int VP = kTile + Q;      // pitch of a dim's row of values, a whole number of words
   __shared__ TilePlan t;
-  __shared__ TS vt[HD * VP];
+  __shared__ __align__(16) TS vt[HD * VP];
   const int tid = threadIdx.x, row0 = blockIdx.x * kTile;
   const int64_t bs = (int64_t)1 << p.st.bs_log2;
-  const int c = tid % LR, d0 = 16 * c;
   const bool keys = p.k.data && (int)blockIdx.y < p.st.n_kv;
   const int h = blockIdx.y % p.st.n_kv;
   if (tid < kTile) plan_tile<X>(p, row0, t);
   __syncthreads();
-  if (!keys) {
-    const int nl = t.n_lead, ns = t.n_single;
-    for (int e = tid; e < nl * HD; e += 256) {
-      const int d = e / nl, r = t.lead[e - d * nl];
-      const int64_t dest = t.dest[r], blk = dest >> p.st.bs_log2, slot = dest & (bs - 1);
-      const u32x4 w = ld16v((const TS*)p.st.v + blk * p.st.v_sb + h * p.st.v_sh + d * bs + slot);
-      TS piece[X];
-      __builtin_memcpy(piece, &w, 16);
-#pragma unroll
-      for (int i = 0; i < X; ++i) vt[d * VP + r + i] = piece[i];
-    }
-    for (int e = tid; e < ns * HD; e += 256) {
-      const int r = t.single[e / HD], d = e % HD;
-      const int64_t dest = t.dest[r], blk = dest >> p.st.bs_log2, slot = dest & (bs - 1);
-      vt[d * VP + r] = ((const TS*)p.st.v)[blk * p.st.v_sb + h * p.st.v_sh + d * bs + slot];
-    }
-    __syncthreads();
-  }
-  for (int r = tid / LR; r < kTile; r += RP) {
-    const int64_t dest = t.dest[r];
-    if (dest < 0) continue;
-    const int64_t blk = dest >> p.st.bs_log2, slot = dest & (bs - 1), row = row0 + r;
-    float x[16], f = 1.f;
-    if constexpr (sizeof(TS) == 1) f = power_of((keys ? p.st.k_exp : p.st.v_exp)[blk * p.st.e_sb + h * p.st.e_sh + slot]);
-    if (keys) {
+  if (keys) {
+    const int c = tid % LR, d0 = 16 * c;
+    for (int r = tid / LR; r < kTile; r += RP) {
+      const int64_t dest = t.dest[r];
+      if (dest < 0) continue;
+      const int64_t blk = dest >> p.st.bs_log2, slot = dest & (bs - 1), row = row0 + r;
+      float x[16], f = 1.f;
+      if constexpr (sizeof(TS) == 1) f = power_of(p.st.k_exp[blk * p.st.e_sb + h * p.st.e_sh + slot]);
       const TS* kb = (const TS*)p.st.k + blk * p.st.k_sb + h * p.st.k_sh;
 #pragma unroll
       for (int q = 0; q < 16 / X; ++q) {
@@ -509,10 +510,50 @@ __global__ __launch_bounds__(256) void cache_read(const CacheParams p) {
         for (int i = 0; i < X; ++i) x[q * X + i] = value_of(piece[i]) * f;
       }
       store16((TI*)p.k.data + row * p.k.row + h * p.k.head + d0, p.k_vec, x);
-    } else {
+    }
+    return;
+  }
+  const int nl = t.n_lead, ns = t.n_single;
+  for (int e = tid; e < nl * HD; e += 256) {
+    const int d = e / nl, r = t.lead[e - d * nl];
+    const int64_t dest = t.dest[r], blk = dest >> p.st.bs_log2, slot = dest & (bs - 1);
+    const u32x4 w = ld16v((const TS*)p.st.v + blk * p.st.v_sb + h * p.st.v_sh + d * bs + slot);
+    if (r % Q == 0) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) x[i] = value_of(vt[(d0 + i) * VP + r]) * f;
-      store16((TI*)p.v.data + row * p.v.row + h * p.v.head + d0, p.v_vec, x);
+      for (int i = 0; i < 4; ++i) reinterpret_cast<uint32_t*>(vt + d * VP + r)[i] = w[i];
+    } else {
+      TS piece[X];
+      __builtin_memcpy(piece, &w, 16);
+#pragma unroll
+      for (int i = 0; i < X; ++i) vt[d * VP + r + i] = piece[i];
+    }
+  }
+  for (int e = tid; e < ns * HD; e += 256) {
+    const int r = t.single[e / HD], d = e % HD;
+    const int64_t dest = t.dest[r], blk = dest >> p.st.bs_log2, slot = dest & (bs - 1);
+    vt[d * VP + r] = ((const TS*)p.st.v)[blk * p.st.v_sb + h * p.st.v_sh + d * bs + slot];
+  }
+  __syncthreads();
+  // a lane takes 8 dims of the Q rows whose values share words
+  for (int e = tid; e < kTile / Q * (HD / 8); e += 256) {
+    const int d0 = 8 * (e % (HD / 8)), r0 = Q * (e / (HD / 8));
+    uint32_t w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = *reinterpret_cast<const uint32_t*>(vt + (d0 + i) * VP + r0);
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      const int64_t dest = t.dest[r0 + q];
+      if (dest < 0) continue;
+      const int64_t blk = dest >> p.st.bs_log2, slot = dest & (bs - 1), row = row0 + r0 + q;
+      float x[8], f = 1.f;
+      if constexpr (sizeof(TS) == 1) f = power_of(p.st.v_exp[blk * p.st.e_sb + h * p.st.e_sh + slot]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        TS part[Q];
+        __builtin_memcpy(part, &w[i], 4);
+        x[i] = value_of(part[q]) * f;
+      }
+      store8((TI*)p.v.data + row * p.v.row + h * p.v.head + d0, p.v_vec, x);
     }
   }
 }
