@@ -453,8 +453,10 @@ __global__ __launch_bounds__(256) void cache_write(const CacheParams p, const sp
 
 // ---------------------------------------------------------------- read
 // The same tiles the other way, a workgroup per KV head for the keys and one for the values: values
-// through LDS, by groups where the tokens make them.  49152 rows of 8 heads to bf16 (head dim 128): from 8-bit 79 us
-// (302 MB, 3.8 TB/s: 1-byte LDS writes and reads of the values' transposition), from bf16 82 (4.9 TB/s).
+// through LDS, by groups where the tokens make them, word by word.  49152 rows of 8 heads to bf16
+// (head dim 128): from 8-bit 70 us (302 MB, 4.3 TB/s; byte by byte through LDS 79), from bf16 79 (403 MB,
+// 5.1 TB/s; 82).  Scattered tokens, whose values lie a byte or two apart: 158 and 324.  More heads a workgroup gain
+// nothing (8-bit: 71, 76, 77, 88 us with 1, 2, 4, 8).
 template <typename TS>
 __device__ __forceinline__ float value_of(TS x) {
   if constexpr (sizeof(TS) == 1) return __builtin_amdgcn_cvt_f32_fp8((int)x.bits, 0);

@@ -165,10 +165,11 @@ TreePlan tree_plan(const sp_tree_config& c, int nodes, int num_cus) {
   const int64_t n = c.max_seq_len, slots = slots_of(num_cus);
   // As many splits as fill the device once, and pieces of at most an eighth of the longest sequence
   // (or 2048 tokens): a batch of long and short sequences takes several rounds, whose ends level
-  // out (64 sequences of 2K-32K tokens, 320 rows: 1315-1345 us in splits of 4096-8192, 1655 of 1024,
-  // 1570 unsplit).  Then up to as many again, until the last round is full: of alike
-  // sequences a round that a third of the device works on costs a whole one (32 of 131072
-  // tokens, 4 rows: 1485 us in 4 splits each, 1.33 rounds; 1350 in 8, 2.67; 1372 in 3, one).
+  // out (64 sequences of 2K-32K tokens, 320 rows: 1160-1176 us in splits of 4096-8192, 1432 of 1024,
+  // 1383 unsplit; 128 of 1K-8K 8-bit tokens, 64 rows: 218 us in splits of 2048, 236 of 1024, 256 unsplit).
+  // Then up to as many again, until the last round is full: of alike sequences a round that a third of
+  // the device works on costs a whole one (32 of 131072 8-bit tokens, 4 rows: 1435 us in 4 splits
+  // each, 1.33 rounds; 1327 in 8, 2.67; 1362 in 3, one; 2184 unsplit).
   const int64_t fill = (n * items + slots - 1) / slots, cap = n / 8 > 2048 ? n / 8 : 2048;
   int64_t len = fill < cap ? fill : cap;
   if (len < kMinSplit) len = kMinSplit;
