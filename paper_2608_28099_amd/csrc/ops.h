@@ -63,7 +63,7 @@ struct TreeParams {
   int nodes, group, max_seq_len;
   float scale_log2;              // the scores' factor times log2(e)
   // the plan: query rows in n_qgroups groups, a workgroup each, of four waves of rows_per_wave (16 or
-  // 32; fp32: groups of 16 rows), r_alloc rows in all; splits of split_len tokens, max_splits of max_seq_len
+  // 32) or of eight that share 16 rows (2; fp32 only), r_alloc rows in all; splits of split_len tokens, max_splits of max_seq_len
   int n_qgroups, rows_per_wave, r_alloc, split_len, max_splits;
   float* o_part;                 // [B][n_kv][max_splits][r_alloc / 16][16 hd], not divided by the sum
   float2* ml_part;               // [B][n_kv][max_splits][r_alloc]: maximum (log2 units), sum

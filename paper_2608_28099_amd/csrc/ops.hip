@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cmath>
+#include <cstdlib>
 #include <cstring>
 #include <functional>
 #include <mutex>
@@ -151,16 +152,21 @@ int64_t slots_of(int num_cus) { return (int64_t)num_cus * 3; }  // three workgro
 void row_groups(const sp_tree_config& c, int nodes, int num_cus, int* rows_per_wave, int* groups) {
   const int rows = nodes * (c.n_q_heads / c.n_kv_heads), g64 = (rows + 63) / 64, g128 = (rows + 127) / 128;
   const bool f32 = c.kv_dtype == SP_F32;
+  if (f32 && (getenv("T_F") ? atoi(getenv("T_F")) : rows <= 16)) {
+    *rows_per_wave = 2;
+    *groups = (rows + 15) / 16;
+    return;
+  }
   const int64_t pieces = (int64_t)c.max_batch * c.n_kv_heads * g128 * (c.max_seq_len / kMinSplit);
   const bool wide = !f32 && rows > 128 && 5 * 128 * g128 <= 6 * 64 * g64 && pieces >= 2 * slots_of(num_cus);
   *rows_per_wave = wide ? 32 : 16;
-  *groups = f32 ? (rows + 15) / 16 : wide ? g128 : g64;
+  *groups = wide ? g128 : g64;
 }
 
 TreePlan tree_plan(const sp_tree_config& c, int nodes, int num_cus) {
   TreePlan p{};
   row_groups(c, nodes, num_cus, &p.rows_per_wave, &p.n_qgroups);
-  p.r_alloc = p.n_qgroups * (c.kv_dtype == SP_F32 ? 16 : 4 * p.rows_per_wave);
+  p.r_alloc = p.n_qgroups * (p.rows_per_wave == 2 ? 16 : 4 * p.rows_per_wave);
   const int64_t items = (int64_t)c.max_batch * c.n_kv_heads * p.n_qgroups;
   const int64_t n = c.max_seq_len, slots = slots_of(num_cus);
   // As many splits as fill the device once, and pieces of at most an eighth of the longest sequence

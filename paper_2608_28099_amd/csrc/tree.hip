@@ -10,7 +10,7 @@
 // scores, the sum and the output of a row stay in the lanes of that row, and the scores that a
 // lane receives of the first product are, as weights, its operand of the second.  For that the
 // keys' tokens go to the rows of the first product in an order of their own (Wave16, Wave32).
-// Units: 32 tokens of bf16 caches and nodes, 64 of 8-bit caches, so that either reads 16 bytes
+// Units: 32 tokens of bf16 caches and nodes, 64 of 8-bit caches, 16 of fp32 (WaveF32), so that each reads 16 bytes
 // per lane at a time.  8-bit keys become bf16 with their exponent, exactly; the values'
 // exponents go to the weights instead, exactly too (a power of two).
 #include <type_traits>
@@ -87,13 +87,23 @@ struct Unit {
   static constexpr int KP = SUB + PAD, VB = NSUB * KP;
   static constexpr int EB = VB + NSUB * SUB;         // exponents: per run 4 words the keys', 4 the values'
   static constexpr int PIECES = EB + (E8 ? 2 * NSUB : 0);
-  static constexpr int IPG = SUB / 64;               // loads of 64 pieces per run's keys, or its values
+  static constexpr int PARTS = 1, IPG = SUB / 64;    // waves that share a run's keys, or its values; loads of 64 pieces each
   // byte offset of piece q of a run from its first token's place in the block
   static __device__ __forceinline__ uint32_t key_off(int q, int bs) { return (uint32_t)((q >> 4) * bs + (q & 15)) * 16u; }
   static __device__ __forceinline__ uint32_t value_off(int q, int bs) {
     if (E8) return (uint32_t)(q * bs);
     return (uint32_t)((16 * (q >> 5) + (q & 15)) * bs * 2 + ((q >> 4) & 1) * 16);
   }
+};
+
+// The image of a unit of fp32: one run of 16 tokens; keys: piece c * 16 + t = dims 4 c .. of token t; values: piece
+// 4 d + e = dim d of tokens 4 e .. 4 e + 3.  Fragments are 1 KB in a row per wave.
+template <int HD>
+struct UnitF32 {
+  static constexpr int NSUB = 1, TOKENS = 16, SUB = 4 * HD, KP = SUB, VB = SUB, EB = 2 * SUB, PIECES = 2 * SUB;
+  static constexpr int PARTS = 2, IPG = SUB / 128;
+  static __device__ __forceinline__ uint32_t key_off(int q, int bs) { return (uint32_t)((q >> 4) * bs + (q & 15)) * 16u; }
+  static __device__ __forceinline__ uint32_t value_off(int q, int bs) { return (uint32_t)((q >> 2) * bs * 4 + (q & 3) * 16); }
 };
 
 // Physical block ids of a split: two windows of kIdWin logical blocks, window w in half w & 1.
@@ -175,7 +185,9 @@ struct RowState {
 // tokens of dim 16 nt + li, side by side in the cache (TPL 8 in bf16 units, 16 in 8-bit ones).
 template <int HD, bool E8>
 struct Wave16 {
-  static constexpr int ROWS = 16, PAD = 4, NC = HD / 32, NT = HD / 16;
+  static constexpr int ROWS = 16, PAD = 4, NC = HD / 32, NT = HD / 16, NODES = 32;
+  typedef bf16 T;
+  typedef Unit<HD, E8, PAD> U;
   RowState<NT, f32x4, 4> st;  // o[nt][r]: dim 16 nt + 4 la + r
   bf16x8 q[NC];
   int li, la;
@@ -320,7 +332,9 @@ struct Wave16 {
 // token m % 4 + 4 (m / 8) of run m / 4 % 2, so that the lane's 16 scores are those of run lh.
 template <int HD, bool E8>
 struct Wave32 {
-  static constexpr int ROWS = 32, PAD = 0, NC = HD / 16, ND = HD / 32;
+  static constexpr int ROWS = 32, PAD = 0, NC = HD / 16, ND = HD / 32, NODES = 32;
+  typedef bf16 T;
+  typedef Unit<HD, E8, PAD> U;
   RowState<ND, f32x16, 16> st;  // o[dt][4 k + r]: dim 32 dt + 8 k + 4 lh + r
   bf16x8 q[NC];
   int lj, lh;
@@ -496,6 +510,108 @@ struct Wave32 {
   }
 };
 
+// A wave of 16 rows with fp32 products (16x16x4): product (j, e) takes dims 16 j + 4 la + e of token and row li, and
+// leaves the lane the scores of tokens 4 la + r of row li, its operands of the second.
+template <int HD, bool>
+struct WaveF32 {
+  static constexpr int ROWS = 16, PAD = 0, NJ = HD / 16, NODES = 16;
+  typedef float T;
+  typedef UnitF32<HD> U;
+  RowState<NJ, f32x4, 4> st;  // o[j][r]: dim 16 j + 4 la + r
+  f32x4 q[NJ];
+  int li, la;
+  __device__ __forceinline__ WaveF32(int lane) : li(lane & 15), la(lane >> 4) { st.clear(); }
+  __device__ __forceinline__ int row() const { return li; }
+  __device__ __forceinline__ void load_queries(const float* p, bool vec) {
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const float* x = p + 16 * j + 4 * la;
+      if (vec) q[j] = *reinterpret_cast<const f32x4*>(x);
+      else q[j] = f32x4{x[0], x[1], x[2], x[3]};
+    }
+  }
+  __device__ __forceinline__ void scores(float (&s)[4], const u32x4* sb) const {
+    f32x4 d0 = f32x4{0.f, 0.f, 0.f, 0.f}, d1 = d0;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const f32x4 k = __builtin_bit_cast(f32x4, sb[(4 * j + la) * 16 + li]);
+      d0 = mfma16x16x4_f32(k[0], q[j][0], d0);
+      d1 = mfma16x16x4_f32(k[1], q[j][1], d1);
+      d0 = mfma16x16x4_f32(k[2], q[j][2], d0);
+      d1 = mfma16x16x4_f32(k[3], q[j][3], d1);
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) s[r] = d0[r] + d1[r];
+  }
+  __device__ __forceinline__ void products(const float (&s)[4], const f32x4 (&v)[NJ]) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) st.o[j] = mfma16x16x4_f32(v[j][r], s[r], st.o[j]);
+  }
+  __device__ __forceinline__ void load_values(f32x4 (&v)[NJ], const u32x4* sb) const {
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) v[j] = __builtin_bit_cast(f32x4, sb[U::VB + (16 * j + li) * 4 + la]);
+  }
+  __device__ __forceinline__ void cached_unit(const u32x4* sb, bool tail, int limit, float scale) {
+    float s[4];
+    scores(s, sb);
+    __builtin_amdgcn_sched_barrier(0);
+    f32x4 v[NJ];
+    load_values(v, sb);
+    if (tail)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (4 * la + r >= limit) {
+          s[r] = -INFINITY;
+#pragma unroll
+          for (int j = 0; j < NJ; ++j) v[j][r] = 0.f;
+        }
+    st.template raise<4, 16>(s, scale);
+    st.weigh(s, scale);
+    products(s, v);
+  }
+  template <typename F>
+  __device__ __forceinline__ void node_unit(const u32x4* sb, uint32_t seen, float scale, bool any_odd, F odd) {
+    float s[4];
+    scores(s, sb);
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (!((seen >> (4 * la + r)) & 1)) s[r] = -INFINITY;
+    st.template raise<4, 16>(s, scale);
+    st.weigh(s, scale);
+    f32x4 v[NJ];
+    load_values(v, sb);
+    products(s, v);
+    if (any_odd)
+      for (int t = 0; t < 16; ++t) {
+        float w = s[0];
+#pragma unroll
+        for (int r = 1; r < 4; ++r) w = (t & 3) == r ? s[r] : w;
+        odd(t, __shfl(w, 16 * (t >> 2) + li));
+      }
+  }
+  __device__ __forceinline__ float sum() const {
+    float l = st.l;
+    l += __shfl_xor(l, 16);
+    return l + __shfl_xor(l, 32);
+  }
+  template <typename F>
+  __device__ __forceinline__ void each4(F f) {
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) f(16 * j + 4 * la, st.o[j]);
+  }
+  template <typename F>
+  __device__ __forceinline__ void add4(F f) {
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) st.o[j][r] = f(16 * j + 4 * la + r, st.o[j][r]);
+  }
+};
+
+__device__ __forceinline__ bool is_finite(float x) { return fabsf(x) <= 3.402823466e38f; }
+
 // Nodes 32 u .. of n into the LDS image of a bf16 unit, by the whole workgroup.  Values that
 // are not finite become 0 there (0 * NaN would carry a hidden node's values into every row);
 // returns whether this lane met one.
@@ -533,6 +649,32 @@ __device__ __forceinline__ bool stage_nodes(const TreeParams& p, u32x4* sb, int 
       const uint32_t a0 = (v[0][d / 2] >> (16 * (d & 1))) & 0xffffu, a1 = (v[1][d / 2] >> (16 * (d & 1))) & 0xffffu;
       uint32_t* piece = (uint32_t*)&sb[L::VB + run * L::SUB + (2 * (dim / 16) + e) * 16 + dim % 16];
       piece[(t & 7) / 2] = a0 | (a1 << 16);
+    }
+  }
+  return odd;
+}
+
+// The same for nodes 16 u .. and a unit of fp32.
+template <int HD, int W>
+__device__ __forceinline__ bool stage_nodes_f32(const TreeParams& p, u32x4* sb, int b, int g, int u, int n, int tid) {
+  using L = UnitF32<HD>;
+  const float* kb = (const float*)p.k.data + (int64_t)b * p.nodes * p.k.row + g * p.k.head;
+  const float* vb = (const float*)p.v.data + (int64_t)b * p.nodes * p.v.row + g * p.v.head;
+  bool odd = false;
+  for (int i = tid; i < 4 * HD; i += 64 * W) {
+    const int c = i % (HD / 4), t = i / (HD / 4), node = 16 * u + t;  // dims 4 c .. of node t
+    f32x4 k = f32x4{0.f, 0.f, 0.f, 0.f}, v = k;
+    if (node < n) {
+      const float *kr = kb + (int64_t)node * p.k.row + 4 * c, *vr = vb + (int64_t)node * p.v.row + 4 * c;
+      k = p.k_vec ? *reinterpret_cast<const f32x4*>(kr) : f32x4{kr[0], kr[1], kr[2], kr[3]};
+      v = p.v_vec ? *reinterpret_cast<const f32x4*>(vr) : f32x4{vr[0], vr[1], vr[2], vr[3]};
+    }
+    sb[c * 16 + t] = __builtin_bit_cast(u32x4, k);
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+      const bool ok = is_finite(v[d]);
+      odd |= !ok;
+      ((float*)&sb[L::VB + 4 * (4 * c + d) + t / 4])[t % 4] = ok ? v[d] : 0.f;
     }
   }
   return odd;
@@ -594,7 +736,8 @@ __device__ __forceinline__ float lse_of(float m, float l) {
 // wave (a wave without rows too).  A sequence's last split takes the nodes as well, first, while its
 // first units arrive.  A sequence of one split is finished here, else its splits leave (m, l) and O
 // for tree_merge.
-// What bounds it (8 KV heads, head dim 128): few rows, the read: 32 sequences of 131072 8-bit tokens, 4 rows each:
+// What bounds it (8 KV heads, head dim 128).  fp32, the matrix cores: 32 sequences of 8000 tokens, 240 rows: 2060 us, 122
+// TFLOP/s of 157 at the nominal clock; 4 rows, the read: 349 us, 6.0 TB/s. few rows, the read: 32 sequences of 131072 8-bit tokens, 4 rows each:
 // 1335 us for 8.7 GB, 6.5 TB/s, where plain reads reach 7.1.  64 rows of 8-bit tokens: the conversions,
 // one per two values and wave, beside both products and the exponentials: 128 sequences of 1K-8K: 220 us, 4.0
 // TB/s and 485 TFLOP/s, matrix cores 27% busy.  320 rows of bf16: 64 sequences of 2K-32K: 1165 us with their join, 830
@@ -605,13 +748,16 @@ constexpr int kWaves = 4;
 template <int HD, bool E8, template <int, bool> class Wave>
 __global__ __launch_bounds__(64 * kWaves, 3) void tree_split(const TreeParams p) {
   using WV = Wave<HD, E8>;
-  using L = Unit<HD, E8, WV::PAD>;
-  constexpr int NSUB = L::NSUB, U = L::TOKENS, IPG = L::IPG, W = kWaves;
+  using L = typename WV::U;
+  using T = typename WV::T;
+  constexpr bool F32 = sizeof(T) == 4;
+  constexpr int NSUB = L::NSUB, U = L::TOKENS, IPG = L::IPG, W = kWaves, NODES = WV::NODES;
   constexpr int NS = 3, D = 2;  // LDS stages, units ahead
-  // A wave loads the keys and values of one run of every unit (8-bit: four runs), or its keys or values (two).
+  // A wave loads the keys and values of one run of every unit (8-bit: four runs), or its keys or values (two), or half
+  // of them (fp32: one).
   constexpr int KIND = NSUB == W ? 2 : 1, LOADS = KIND * IPG + (E8 ? 1 : 0);
-  static_assert(KIND * W == 2 * NSUB && D * LOADS < 64, "every run once, and the loads in flight");
-  static_assert(L::PIECES >= Unit<HD, false, WV::PAD>::PIECES, "a stage holds a unit of nodes");
+  static_assert(KIND * W == 2 * NSUB * L::PARTS && D * LOADS < 64, "every run once, and the loads in flight");
+  static_assert(F32 || L::PIECES >= Unit<HD, false, WV::PAD>::PIECES, "a stage holds a unit of nodes");
   __shared__ u32x4 stage[NS][L::PIECES];
   __shared__ int blk_ids[2][kIdWin];
   __shared__ int odd_values[W];
@@ -633,10 +779,10 @@ __global__ __launch_bounds__(64 * kWaves, 3) void tree_split(const TreeParams p)
 
   WV wv(lane);
   const int row = min(row0 + wv.row(), rows - 1), node = row / p.group, head = g * p.group + row % p.group;
-  wv.load_queries((const bf16*)p.q.data + ((int64_t)b * p.nodes + node) * p.q.row + (int64_t)head * p.q.head, p.q_vec);
+  wv.load_queries((const T*)p.q.data + ((int64_t)b * p.nodes + node) * p.q.row + (int64_t)head * p.q.head, p.q_vec);
 
   const StoreArg& c = p.st;
-  constexpr int ESZ = E8 ? 1 : 2;
+  constexpr int ESZ = E8 ? 1 : sizeof(T);
   const int bs = 1 << c.bs_log2, nunits = (t1 - t0 + U - 1) / U, lastu = nunits - 1;
   const int lb0 = t0 >> c.bs_log2, nlb = t1 > t0 ? ((t1 - 1) >> c.bs_log2) - lb0 + 1 : 0;
   const int* bt_row = c.block_table ? c.block_table + (int64_t)b * c.mbps + lb0 : nullptr;
@@ -649,11 +795,14 @@ __global__ __launch_bounds__(64 * kWaves, 3) void tree_split(const TreeParams p)
     const int i = j * 64 * W + tid;
     ids[j] = !bt_row ? b * c.mbps + lb0 + i : i < nlb ? bt_row[i] : 0;
   }
-  if (last) {
-    const bool odd = stage_nodes<HD, W, WV::PAD>(p, stage[D], b, g, 0, n, tid);
+  auto nodes_to_stage = [&](int u) __attribute__((always_inline)) {
+    bool odd;
+    if constexpr (F32) odd = stage_nodes_f32<HD, W>(p, stage[D], b, g, u, n, tid);
+    else odd = stage_nodes<HD, W, WV::PAD>(p, stage[D], b, g, u, n, tid);
     const bool any = __any(odd);
     if (lane == 0) odd_values[wave] = any;
-  }
+  };
+  if (last) nodes_to_stage(0);
 #pragma unroll
   for (int j = 0; j < IDS; ++j) (&blk_ids[0][0])[j * 64 * W + tid] = ids[j];
   auto load_window = [&](int w) __attribute__((always_inline)) {
@@ -664,7 +813,7 @@ __global__ __launch_bounds__(64 * kWaves, 3) void tree_split(const TreeParams p)
     }
   };
   // This wave's run of a unit, and what it loads of it: first kind 0 keys, 1 values.
-  const int run = wave * NSUB / W, kind0 = KIND == 1 ? wave & 1 : 0;
+  const int run = wave * NSUB / W, kind0 = KIND == 1 ? wave & 1 : 0, part = L::PARTS == 1 ? 0 : wave >> 1;
   uint32_t lane_off[KIND][IPG];
   const char* kind_base[KIND];  // a run's place: kind_base + block * block_step + (slot << slot_shift)
   uint64_t block_step[KIND];
@@ -676,11 +825,11 @@ __global__ __launch_bounds__(64 * kWaves, 3) void tree_split(const TreeParams p)
   for (int k = 0; k < KIND; ++k) {
     const bool v = kind0 + k;
 #pragma unroll
-    for (int j = 0; j < IPG; ++j) lane_off[k][j] = v ? L::value_off(64 * j + lane, bs) : L::key_off(64 * j + lane, bs);
+    for (int j = 0; j < IPG; ++j) lane_off[k][j] = v ? L::value_off(64 * (IPG * part + j) + lane, bs) : L::key_off(64 * (IPG * part + j) + lane, bs);
     kind_base[k] = v ? (const char*)c.v + g * c.v_sh * ESZ : (const char*)c.k + g * c.k_sh * ESZ;
     block_step[k] = (uint64_t)(v ? c.v_sb : c.k_sb) * ESZ;
-    slot_shift[k] = v ? (E8 ? 0 : 1) : 4;
-    piece0[k] = v ? L::VB + run * L::SUB : run * L::KP;
+    slot_shift[k] = v ? (E8 ? 0 : F32 ? 2 : 1) : 4;
+    piece0[k] = (v ? L::VB + run * L::SUB : run * L::KP) + 64 * IPG * part;
     stream[k] = p.n_qgroups == 1 && (!v || bs * ESZ <= 64);
   }
   const uint8_t* exp_base = lane & 4 ? c.v_exp : c.k_exp;  // 8-bit: lanes 0..3 the keys' exponents, 4..7 the values'
@@ -732,25 +881,24 @@ __global__ __launch_bounds__(64 * kWaves, 3) void tree_split(const TreeParams p)
     if (lastu > 0) issue(1);
   }
   if (last)  // the nodes, from the stage that unit D will take
-    for (int u = 0; 32 * u < n; ++u) {
+    for (int u = 0; NODES * u < n; ++u) {
       if (u > 0) {
         lds_barrier();
-        const bool odd = stage_nodes<HD, W, WV::PAD>(p, stage[D], b, g, u, n, tid);
-        const bool any = __any(odd);
-        if (lane == 0) odd_values[wave] = any;
+        nodes_to_stage(u);
         lds_barrier();
       }
       if (!active) continue;
       bool odd = false;
 #pragma unroll
       for (int w = 0; w < W; ++w) odd |= odd_values[w] != 0;
-      const bf16* vb = (const bf16*)p.v.data + (int64_t)b * p.nodes * p.v.row + g * p.v.head;
+      const T* vb = (const T*)p.v.data + (int64_t)b * p.nodes * p.v.row + g * p.v.head;
+      const uint32_t seen = seen_word(p, b, node, NODES * u / 32, n) >> (NODES * u % 32);
       // the values that are not finite, kept out of the products, reach the rows that see them alone
-      wv.node_unit(stage[D], seen_word(p, b, node, u, n), p.scale_log2, odd, [&](int t, float w) {
-        if (32 * u + t >= n) return;
+      wv.node_unit(stage[D], seen, p.scale_log2, odd, [&](int t, float w) {
+        if (NODES * u + t >= n) return;
         wv.add4([&](int d, float o) {
-          const float x = to_f32(vb[(int64_t)(32 * u + t) * p.v.row + d]);
-          return w != 0.f && !(fabsf(x) <= 3.389531389e38f) ? fmaf(w, x, o) : o;
+          const float x = to_f32(vb[(int64_t)(NODES * u + t) * p.v.row + d]);
+          return w != 0.f && !is_finite(x) ? fmaf(w, x, o) : o;
         });
       });
     }
@@ -774,10 +922,11 @@ __global__ __launch_bounds__(64 * kWaves, 3) void tree_split(const TreeParams p)
     if (!live) return;
     if (p.lse && first) p.lse[((int64_t)b * p.nodes + node) * (p.st.n_kv * p.group) + head] = lse_of(wv.st.m, l);
     const float inv = l == 0.f ? 0.f : 1.0f / l;
-    bf16* o = (bf16*)p.out.data + ((int64_t)b * p.nodes + node) * p.out.row + (int64_t)head * p.out.head;
+    T* o = (T*)p.out.data + ((int64_t)b * p.nodes + node) * p.out.row + (int64_t)head * p.out.head;
+    typedef T T4 __attribute__((ext_vector_type(4)));
     wv.each4([&](int d, f32x4 x) {
-      const bf16x4 y{(bf16)(x[0] * inv), (bf16)(x[1] * inv), (bf16)(x[2] * inv), (bf16)(x[3] * inv)};
-      if (p.o_vec) *reinterpret_cast<bf16x4*>(o + d) = y;
+      const T4 y{from_f32<T>(x[0] * inv), from_f32<T>(x[1] * inv), from_f32<T>(x[2] * inv), from_f32<T>(x[3] * inv)};
+      if (p.o_vec) *reinterpret_cast<T4*>(o + d) = y;
       else
 #pragma unroll
         for (int r = 0; r < 4; ++r) o[d + r] = y[r];
@@ -876,13 +1025,10 @@ __global__ __launch_bounds__(256) void tree_merge(const TreeParams p) {
 }
 
 // ---------------------------------------------------------------- fp32
-// The same rows with fp32 products: S^T = K Q^T, lane (li, la) holding dims 16 j + 4 la + e
-// of token and row li, then O^T += V^T P^T with the scores of row li that the lane already
-// has (tokens 4 la + r), so the running softmax needs no exchange but its maximum's.  One
-// workgroup of 8 waves per (query tile, KV head; split; sequence); the waves take every
-// eighth step of 16 tokens, cached ones and then, in the last split, nodes, straight from
-// memory, and join through LDS in their order.  4 sequences of 256 tokens, 4 nodes: 8 us, bound by the chain of
-// loads, steps and join (one wave per tile: 24).
+// The same rows with fp32 products, lane (li, la) as in WaveF32, for calls of few workgroups: one workgroup of 8 waves
+// per (query tile, KV head; split; sequence); the waves take every eighth step of 16 tokens, cached ones and
+// then, in the last split, nodes, straight from memory, and join through LDS in their order.  4 sequences of 256
+// tokens, 4 nodes of 2 heads: 8 us, bound by the chain of loads, steps and join (staged through LDS, as larger calls are: 18).
 constexpr int kF32Waves = 8;
 
 template <int HD>
@@ -1038,8 +1184,8 @@ __global__ __launch_bounds__(64 * kF32Waves) void tree_split_f32(const TreeParam
 hipError_t launch_tree(const TreeParams& p, int storage, int hd, hipStream_t s) {
   const int rows = p.nodes * p.group;
   hipError_t e;
-  if (storage == SP_F32) {
-    if (p.split_len % 16 || (rows + 15) / 16 * 16 > p.r_alloc) return hipErrorInvalidValue;
+  if (p.rows_per_wave == 2) {
+    if (storage != SP_F32 || p.split_len % 16 || (rows + 15) / 16 * 16 > p.r_alloc) return hipErrorInvalidValue;
     const dim3 grid(p.st.n_kv * ((rows + 15) / 16), p.max_splits, p.st.batch), block(64 * kF32Waves);
     if (hd == 128) hipLaunchKernelGGL((tree_split_f32<128>), grid, block, 0, s, p);
     else hipLaunchKernelGGL((tree_split_f32<64>), grid, block, 0, s, p);
@@ -1048,12 +1194,18 @@ hipError_t launch_tree(const TreeParams& p, int storage, int hd, hipStream_t s) 
     if (p.split_len % 64 || p.r_alloc < rows || p.r_alloc != p.n_qgroups * p.rows_per_wave * kWaves) return hipErrorInvalidValue;
     const dim3 grid(p.st.n_kv * p.n_qgroups, p.max_splits, p.st.batch), block(64 * kWaves);
     const bool e8 = storage == SP_E4M3;
+    if (storage == SP_F32) {
+      if (p.rows_per_wave != 16) return hipErrorInvalidValue;
+      if (hd == 128) hipLaunchKernelGGL((tree_split<128, false, WaveF32>), grid, block, 0, s, p);
+      else hipLaunchKernelGGL((tree_split<64, false, WaveF32>), grid, block, 0, s, p);
+    } else {
 #define SP_TREE(HD_, E8_, ROWS_)                                                                   \
   if (hd == HD_ && e8 == E8_ && p.rows_per_wave == ROWS_)                                          \
     hipLaunchKernelGGL((tree_split<HD_, E8_, Wave##ROWS_>), grid, block, 0, s, p);
     SP_TREE(128, false, 16) SP_TREE(128, false, 32) SP_TREE(128, true, 16) SP_TREE(128, true, 32)
     SP_TREE(64, false, 16) SP_TREE(64, false, 32) SP_TREE(64, true, 16) SP_TREE(64, true, 32)
 #undef SP_TREE
+    }
     e = hipGetLastError();
   }
   if (e != hipSuccess || p.max_splits == 1) return e;
