@@ -494,7 +494,7 @@ typedef struct sp_tree_config {
   int32_t dtype;                  /* SP_F32 (with an SP_F32 cache) or SP_BF16 (SP_BF16 or SP_E4M3): q, k, v and out */
   int32_t kv_dtype;               /* storage of the cache */
   int32_t max_nodes;              /* 1..256 */
-  int32_t max_batch;
+  int32_t max_batch;              /* the launch is planned for it and max_seq_len: near a call's own, best */
   int32_t max_seq_len;            /* longest context a call may pass, up to 2^30; lengths are clamped to [0, max_seq_len] */
   float scale;                    /* factor on the scores; 0: 1 / sqrt(head_dim) */
   int32_t reserved;               /* 0 */

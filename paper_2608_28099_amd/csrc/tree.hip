@@ -737,7 +737,7 @@ __device__ __forceinline__ float lse_of(float m, float l) {
 // first units arrive.  A sequence of one split is finished here, else its splits leave (m, l) and O
 // for tree_merge.
 // What bounds it (8 KV heads, head dim 128).  fp32, the matrix cores: 32 sequences of 8000 tokens, 240 rows: 2060 us, 122
-// TFLOP/s of 157 at the nominal clock; 4 rows, the read: 349 us, 6.0 TB/s. few rows, the read: 32 sequences of 131072 8-bit tokens, 4 rows each:
+// TFLOP/s of 157 at the nominal clock; 4 rows, the read: 349 us, 6.0 TB/s.  Few rows, the read: 32 sequences of 131072 8-bit tokens, 4 rows each:
 // 1335 us for 8.7 GB, 6.5 TB/s, where plain reads reach 7.1.  64 rows of 8-bit tokens: the conversions,
 // one per two values and wave, beside both products and the exponentials: 128 sequences of 1K-8K: 220 us, 4.0
 // TB/s and 485 TFLOP/s, matrix cores 27% busy.  320 rows of bf16: 64 sequences of 2K-32K: 1165 us with their join, 830

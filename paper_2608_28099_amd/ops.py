@@ -142,6 +142,8 @@ def rotary(rot, positions, q, k=None, out=None, k_out=None, transpose=False, str
         raise ValueError("out must have q's shape")
     qr, outr = _rows(q, "q", hd, dtype, dev, n), _rows(out, "out", hd, dtype, dev, n)
     kr = k_outr = None
+    if k is None and k_out is not None:
+        raise ValueError("k_out without k")
     if k is not None:
         if k_out is None:
             k_out = _empty_like(k, stream)
@@ -346,7 +348,8 @@ def tree_attention(cache: PagedCache, seq_lens, q, k, v, mask=None, counts=None,
 
 
 def tree_workspace_bytes(cache: PagedCache, n_q_heads, dtype, nodes, batch=None, max_seq_len=None):
-    """Bytes of workspace that tree_attention needs for calls of at most these sizes (0: not supported)."""
+    """Bytes of workspace that tree_attention needs for calls of at most these nodes, with this batch and
+    max_seq_len, which plan the launch (0: not supported)."""
     return binding.load().sp_probe_tree_workspace_bytes(
         _tree_config(cache, n_q_heads, dtype, nodes, cache.batch if batch is None else batch,
                      cache.capacity if max_seq_len is None else max_seq_len, 0.0))

@@ -253,3 +253,110 @@ def test_results_on_a_given_stream_use_that_streams_memory(dev):
     assert y.data_ptr() != at
     torch.cuda.synchronize()
     assert float(total) == 2.0 * q.numel() and torch.equal(y, ref)
+
+
+@pytest.mark.parametrize("store", STORES)
+def test_calls_without_rows(dev, store):
+    dtype = torch.float32 if store == torch.float32 else torch.bfloat16
+    cache = make_cache(dev, store, (20, 5), 2, 64, 16, fill=1.0)
+    before = [t.clone() for t in (cache.k, cache.v)]
+    none = torch.empty(0, dtype=torch.int32, device=dev)
+    x = torch.empty((0, 2, 64), dtype=dtype, device=dev)
+    rot = ops.make_rotary(64)
+    assert ops.rotary(rot, none, x).shape == x.shape
+    assert [t.shape for t in ops.rotary(rot, none, x, x)] == [x.shape, x.shape]
+    ops.cache_write(cache, none, none, x, x)
+    ops.cache_write(cache, none, none, torch.ones((3, 2, 64), dtype=dtype, device=dev), torch.ones((3, 2, 64), dtype=dtype, device=dev),
+                    src_rows=none, rotary=rot)
+    ids = torch.zeros(3, dtype=torch.int32, device=dev)
+    ops.cache_write(cache, ids, ids, x, x, src_rows=ids)   # no row to take: nothing is written
+    assert ops.cache_read(cache, none, none, dtype)[0].shape == x.shape
+    for a, b in zip(before, (cache.k, cache.v)):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+    empty = ops.PagedCache(cache.k, cache.v, 16, torch.empty((0, 4), dtype=torch.int32, device=dev), cache.k_exponents, cache.v_exponents)
+    q = torch.empty((0, 3, 4, 64), dtype=dtype, device=dev)
+    assert ops.tree_attention(empty, none, q, q[:, :, :2], q[:, :, :2]).shape == q.shape
+
+
+@pytest.mark.parametrize("store", STORES)
+@pytest.mark.parametrize("which", ["k", "v"])
+def test_one_side_read_into_padded_rows(dev, store, which):
+    """Keys or values alone, into rows that are not 16-byte aligned, some tokens several times, some rows skipped."""
+    gen = seeded(70)
+    cache = make_cache(dev, store, (90, 33), 3, 64, 16, 1)
+    seq, pos = tokens((90, 33))
+    x = torch.randn((len(seq), 6, 64), generator=gen).to(dev)
+    ops.cache_write(cache, seq.to(dev), pos.to(dev), x[:, :3], x[:, 3:])
+    order = torch.cat([torch.arange(60), torch.tensor([5, 5, 5, 122, 0]), torch.arange(20, 60)])
+    s, p = seq[order].to(dev), pos[order].to(dev)
+    s[7], p[9] = -1, 1 << 30
+    for dtype in (torch.float32, torch.bfloat16):
+        out = torch.full((len(order), 3, 67), 7.0, dtype=dtype, device=dev)
+        got = ops.cache_read(cache, s, p, **{which: out[..., :64]})
+        assert got[0 if which == "k" else 1].data_ptr() == out.data_ptr() and got[1 if which == "k" else 0] is None
+        whole = ops.cache_read(cache, seq.to(dev), pos.to(dev), dtype)[0 if which == "k" else 1][order.to(dev)]
+        live = torch.ones(len(order), dtype=torch.bool)
+        live[7] = live[9] = False
+        assert torch.equal(out[live][..., :64], whole[live]) and torch.all(out[~live] == 7.0) and torch.all(out[..., 64:] == 7.0)
+
+
+@pytest.mark.parametrize("store", STORES)
+@pytest.mark.parametrize("lens,t,nq,nkv,hd,block", [
+    ((300, 7), 256, 32, 1, 64, 16),        # 8192 query rows
+    ((20,), 1, 4096, 4096, 64, 16),        # the most heads
+    ((20, 0), 3, 4096, 2, 64, 16),         # 2048 heads on one
+    ((5000, 1, 4096), 9, 4, 2, 128, 4096)])
+def test_sizes_at_their_limits(dev, store, lens, t, nq, nkv, hd, block):
+    c = Tree(dev, store, lens, t, nq, nkv, hd, block, seed=71)
+    c.check(*run(c))
+
+
+def test_calls_from_several_threads(dev):
+    import threading
+    c = Tree(dev, torch.bfloat16, (600, 31), 9, 8, 2, 128, 16, seed=72)
+    ref, _ = run(c)
+    q, k, v = c.qkv()
+    mask = words_of(c.see).to(dev)
+    rot = ops.make_rotary(128)
+    pos = torch.arange(18, dtype=torch.int32, device=dev)
+    turned = ops.rotary(rot, pos, q.reshape(18, 8, 128))
+    torch.cuda.synchronize()
+    bad = []
+
+    def work():
+        side = torch.cuda.Stream()
+        with torch.cuda.stream(side):
+            for _ in range(20):
+                a = ops.tree_attention(c.cache, c.seq_lens, q, k, v, mask=mask, max_seq_len=600)
+                b = ops.rotary(rot, pos, q.reshape(18, 8, 128))
+                side.synchronize()
+                if not (torch.equal(a, ref) and torch.equal(b, turned)):
+                    bad.append(1)
+
+    threads = [threading.Thread(target=work) for _ in range(3)]
+    for th in threads:
+        th.start()
+    for th in threads:
+        th.join()
+    assert not bad
+
+
+def test_refusals_of_tensors(dev):
+    rot = ops.make_rotary(64)
+    x = torch.zeros((2, 3, 64), device=dev)
+    pos = torch.zeros(2, dtype=torch.int32, device=dev)
+    for args, kw in (((rot, pos.long(), x), {}), ((rot, pos, x.half()), {}), ((rot, pos, x[..., ::2]), {}), ((rot, pos.cpu(), x), {}),
+                     ((rot, pos, x), dict(k_out=x)), ((rot, pos, x), dict(out=x[:1])), ((rot, pos[:1], x), {})):
+        with pytest.raises(ValueError):
+            ops.rotary(*args, **kw)
+    c = Tree(dev, torch.bfloat16, (20, 3), 4, 4, 2, 64, 16)
+    q, k, v = c.qkv()
+    for kw in (dict(seq_lens=c.seq_lens[:1]), dict(q=q[:1]), dict(k=k[:, :, :1]), dict(scale=-1.0), dict(scale=math.inf), dict(scale=0.0),
+               dict(mask=torch.zeros((2, 3, 1), dtype=torch.int32, device=dev)), dict(lse=torch.zeros(2, 4, 4)),
+               dict(workspace=torch.zeros(64, device=dev)), dict(counts=torch.zeros(3, dtype=torch.int32, device=dev))):
+        a = dict(dict(cache=c.cache, seq_lens=c.seq_lens, q=q, k=k, v=v), **kw)
+        with pytest.raises(ValueError):
+            ops.tree_attention(**a)
+    for kw in (dict(max_seq_len=c.cache.capacity + 1), dict(max_seq_len=-1), dict(workspace=torch.zeros(16, dtype=torch.uint8, device=dev))):
+        with pytest.raises(binding.ProbeError):
+            ops.tree_attention(c.cache, c.seq_lens, q, k, v, **kw)
