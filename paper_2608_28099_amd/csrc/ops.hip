@@ -3,7 +3,6 @@
 #include <hip/hip_runtime.h>
 
 #include <cmath>
-#include <cstdlib>
 #include <cstring>
 #include <functional>
 #include <mutex>
@@ -141,8 +140,12 @@ size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 constexpr int kMinSplit = 256;  // tokens
 int64_t slots_of(int num_cus) { return (int64_t)num_cus * 3; }  // three workgroups per compute unit, by LDS
 
-// Rows of a wave, and workgroups (of four waves) that the rows of a KV head take; fp32: 16 rows a
-// workgroup.  A wave of 32 rows reads half as much from LDS per row and converts 8-bit keys and values half as often,
+// Rows of a wave, and workgroups that the rows of a KV head take.  Workgroups of four waves, 16 or 32 rows each;
+// fp32, while pieces of kMinSplit tokens and 16 rows are two per compute unit at most, of eight waves for 16 rows (2 "rows a
+// wave"), which have a shorter way to the first result (8 KV heads, head dim 128, eight waves / four of 16 rows, in us: one
+// sequence of 2000 tokens, 4 rows 15.9 / 28.6, 240 rows 59 / 43; 4 of 8000, 4 rows 69 / 53; 48 of 2000, 64 rows
+// 566 / 242; 32 of 8000, 240 rows 4110 / 2061).
+// A wave of 32 rows reads half as much from LDS per row and converts 8-bit keys and values half as often,
 // but one group of 128 rows in place of two of 64 leaves half as many to spread over the device.  So
 // waves of 32 from 129 rows on, where padding to 128 adds at most a fifth and pieces of kMinSplit tokens
 // would still fill the device twice.  Measured (8 KV heads, head dim 128, in us, 16 rows a wave / 32): 64 sequences of 6000
@@ -152,7 +155,8 @@ int64_t slots_of(int num_cus) { return (int64_t)num_cus * 3; }  // three workgro
 void row_groups(const sp_tree_config& c, int nodes, int num_cus, int* rows_per_wave, int* groups) {
   const int rows = nodes * (c.n_q_heads / c.n_kv_heads), g64 = (rows + 63) / 64, g128 = (rows + 127) / 128;
   const bool f32 = c.kv_dtype == SP_F32;
-  if (f32 && (getenv("T_F") ? atoi(getenv("T_F")) : rows <= 16)) {
+  const int64_t splits = c.max_seq_len < kMinSplit ? 1 : c.max_seq_len / kMinSplit;
+  if (f32 && (int64_t)c.max_batch * c.n_kv_heads * ((rows + 15) / 16) * splits <= 2 * num_cus) {
     *rows_per_wave = 2;
     *groups = (rows + 15) / 16;
     return;
