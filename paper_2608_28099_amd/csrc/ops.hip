@@ -145,13 +145,13 @@ int64_t slots_of(int num_cus) { return (int64_t)num_cus * 3; }  // three workgro
 // wave"), which have a shorter way to the first result (8 KV heads, head dim 128, eight waves / four of 16 rows, in us: one
 // sequence of 2000 tokens, 4 rows 15.9 / 28.6, 240 rows 59 / 43; 4 of 8000, 4 rows 69 / 53; 48 of 2000, 64 rows
 // 566 / 242; 32 of 8000, 240 rows 4110 / 2061).
-// A wave of 32 rows reads half as much from LDS per row and converts 8-bit keys and values half as often,
-// but one group of 128 rows in place of two of 64 leaves half as many to spread over the device.  So
-// waves of 32 from 129 rows on, where padding to 128 adds at most a fifth and pieces of kMinSplit tokens
-// would still fill the device twice.  Measured (8 KV heads, head dim 128, in us, 16 rows a wave / 32): 64 sequences of 6000
-// tokens, bf16: 240 rows 607 / 533, 320 rows 756 / 684, 480 rows 1113 / 949; 8-bit: 637 / 617, 801 / 805, 1195 / 1117; 160
-// rows, padded to 192 or 256: 487 / 460 and 490 / 517; 16 of 4000, 160 rows: 76 / 86 and 96 / 105, 128 rows: 63 / 77 and
-// 73 / 80; 240 rows, 4 of 8000: 56.6 / 57.3 and 69.6 / 68.0, one of 2000: 20.2 / 23.6 and 20.9 / 26.4.
+// A wave of 32 rows reads half as much from LDS per row, but one group of 128 rows in place of two of 64 leaves
+// half as many to spread over the device.  So waves of 32 for bf16 caches (whose waves of 16 are bound by LDS) from 129
+// rows on, where padding to 128 adds at most a fifth and pieces of kMinSplit tokens would still fill the device
+// twice.  Measured (in us, 16 rows a wave / 32): 64 sequences of 6000 tokens: 240 rows 607 / 523, 320 rows 756 / 665,
+// 480 rows 1113 / 937; 160 rows, padded to 192 or 256: 487 / 460; 16 of 4000, 160 rows: 76 / 86, 128 rows: 63 / 77;
+// 240 rows, 4 of 8000: 56.6 / 55.1, one of 2000: 20.2 / 23.6.  8-bit, 64 of 6000: 240 rows 626 / 652, 320 rows 794 / 873,
+// 480 rows 1189 / 1181, and two waves of 32 rows for every 64 (each half of a unit's tokens): 648, 811, 1212.
 void row_groups(const sp_tree_config& c, int nodes, int num_cus, int* rows_per_wave, int* groups) {
   const int rows = nodes * (c.n_q_heads / c.n_kv_heads), g64 = (rows + 63) / 64, g128 = (rows + 127) / 128;
   const bool f32 = c.kv_dtype == SP_F32;
@@ -162,7 +162,7 @@ void row_groups(const sp_tree_config& c, int nodes, int num_cus, int* rows_per_w
     return;
   }
   const int64_t pieces = (int64_t)c.max_batch * c.n_kv_heads * g128 * (c.max_seq_len / kMinSplit);
-  const bool wide = !f32 && rows > 128 && 5 * 128 * g128 <= 6 * 64 * g64 && pieces >= 2 * slots_of(num_cus);
+  const bool wide = c.kv_dtype == SP_BF16 && rows > 128 && 5 * 128 * g128 <= 6 * 64 * g64 && pieces >= 2 * slots_of(num_cus);
   *rows_per_wave = wide ? 32 : 16;
   *groups = wide ? g128 : g64;
 }

@@ -325,14 +325,14 @@ struct Wave16 {
   }
 };
 
-// A wave of 32 rows on 32x32x16 products: each fragment that it reads from LDS serves twice the rows.
-// Lane (lj, lh) = (lane % 32, lane / 32) belongs to row lj.  bf16 units: row m of the first product is
-// token 16 (m / 16) + 8 (m / 4 % 2) + 4 (m / 8 % 2) + m % 4, so that score i of the lane is token
-// 16 (i / 8) + 8 lh + i % 8: eight tokens of each run.  8-bit units, 32 tokens (two runs) at a time: row m is
-// token m % 4 + 4 (m / 8) of run m / 4 % 2, so that the lane's 16 scores are those of run lh.
+// A wave of 32 rows on 32x32x16 products, of bf16 caches: each fragment that it reads from LDS serves twice the
+// rows.  Lane (lj, lh) = (lane % 32, lane / 32) belongs to row lj.  Row m of the first product is token
+// 16 (m / 16) + 8 (m / 4 % 2) + 4 (m / 8 % 2) + m % 4 of the unit, so that score i of the lane is token
+// 16 (i / 8) + 8 lh + i % 8: eight tokens of each run.
 template <int HD, bool E8>
 struct Wave32 {
   static constexpr int ROWS = 32, PAD = 0, NC = HD / 16, ND = HD / 32, NODES = 32;
+  static_assert(!E8, "bf16 units");
   typedef bf16 T;
   typedef Unit<HD, E8, PAD> U;
   RowState<ND, f32x16, 16> st;  // o[dt][4 k + r]: dim 32 dt + 8 k + 4 lh + r
@@ -340,12 +340,10 @@ struct Wave32 {
   int lj, lh;
   __device__ __forceinline__ Wave32(int lane) : lj(lane & 31), lh(lane >> 5) { st.clear(); }
   __device__ __forceinline__ int row() const { return lj; }
-  // product c takes dims 8 (2 c + lh) .. (bf16 keys), or with 8-bit keys, whose 16 bytes hold 16 dims, the half
-  // c % 2 of piece 2 (c / 2) + lh; the nodes' products follow the same order
-  __device__ __forceinline__ int dims(int c) const { return E8 ? 16 * (2 * (c / 2) + lh) + 8 * (c % 2) : 8 * (2 * c + lh); }
+  // product c takes dims 8 (2 c + lh) ..
   __device__ __forceinline__ void load_queries(const bf16* p, bool vec) {
 #pragma unroll
-    for (int c = 0; c < NC; ++c) q[c] = __builtin_bit_cast(bf16x8, row8(p + dims(c), vec));
+    for (int c = 0; c < NC; ++c) q[c] = __builtin_bit_cast(bf16x8, row8(p + 8 * (2 * c + lh), vec));
   }
   static __device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
@@ -355,13 +353,12 @@ struct Wave32 {
     using L = Unit<HD, false, PAD>;
     const int at = (lj >> 4) * L::KP + 8 * ((lj >> 2) & 1) + 4 * ((lj >> 3) & 1) + (lj & 3);
     f32x16 d;
-    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int i = 0; i < 16; ++i) d[i] = 0.f;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
       if (c == NC / 2) __builtin_amdgcn_sched_barrier(0);  // (all keys at once take too many registers)
-      d = mfma(__builtin_bit_cast(bf16x8, sb[at + dims(c) / 8 * 16]), q[c], d);
+      d = mfma(__builtin_bit_cast(bf16x8, sb[at + (2 * c + lh) * 16]), q[c], d);
     }
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = d[i];
@@ -383,90 +380,36 @@ struct Wave32 {
   }
 
   __device__ __forceinline__ void cached_unit(const u32x4* sb, bool tail, int limit, float scale) {
-    using L = Unit<HD, E8, PAD>;
     float s[16];
-    if constexpr (!E8) {
-      bf16_scores(s, sb);
-      __builtin_amdgcn_s_setprio(0);
-      __builtin_amdgcn_sched_barrier(0);
-      u32x4 v[ND];
+    __builtin_amdgcn_s_setprio(1);
+    bf16_scores(s, sb);
+    __builtin_amdgcn_s_setprio(0);
+    __builtin_amdgcn_sched_barrier(0);
+    u32x4 v[ND];
 #pragma unroll
-      for (int dt = 0; dt < ND; ++dt) v[dt] = bf16_values(sb, dt, 0);
-      if (tail) {
-        int lim = limit;
-        asm volatile("" : "+s"(lim));  // (keeps the masks a branch that whole units skip)
+    for (int dt = 0; dt < ND; ++dt) v[dt] = bf16_values(sb, dt, 0);
+    if (tail) {
+      int lim = limit;
+      asm volatile("" : "+s"(lim));  // (keeps the masks a branch that whole units skip)
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (16 * (i / 8) + 8 * lh + i % 8 >= lim) s[i] = -INFINITY;
-        clear_tail(v, lim - 8 * lh);
-      }
-      st.template raise<16, 32>(s, scale);
-      st.weigh(s, scale);
-      __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const bf16x8 p = weights8(s + 8 * t);
-#pragma unroll
-        for (int dt = 0; dt < ND; ++dt) st.o[dt] = mfma(__builtin_bit_cast(bf16x8, v[dt]), p, st.o[dt]);
-        if (t) break;
-#pragma unroll
-        for (int dt = 0; dt < ND; ++dt) v[dt] = bf16_values(sb, dt, 1);
-        if (tail) clear_tail(v, limit - 16 - 8 * lh);
-      }
-      __builtin_amdgcn_s_setprio(0);
-    } else {
-#pragma unroll
-      for (int w2 = 0; w2 < 2; ++w2) {
-        if (tail && 32 * w2 >= limit) break;
-        const int run = 2 * w2 + ((lj >> 2) & 1), slot = (lj & 3) + 4 * (lj >> 3);
-        const uint32_t ek = ((const uint32_t*)&sb[L::EB + 2 * run])[slot >> 2];
-        const float f = exponent_scale((ek >> (8 * (slot & 3))) & 0xffu);
-        f32x16 d;
-        __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) d[i] = 0.f;
-#pragma unroll
-        for (int c = 0; c < NC / 2; ++c) {
-          const u32x4 w = sb[run * L::KP + (2 * c + lh) * 16 + slot];
-          d = mfma(from_e4m3(w[0], w[1], f), q[2 * c], d);
-          d = mfma(from_e4m3(w[2], w[3], f), q[2 * c + 1], d);
-        }
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = d[i];
-        __builtin_amdgcn_s_setprio(0);
-        __builtin_amdgcn_sched_barrier(0);
-        const int vrun = 2 * w2 + lh;  // the run of the lane's weights
-        u32x4 v[ND], e = sb[L::EB + 2 * vrun + 1];
-#pragma unroll
-        for (int dt = 0; dt < ND; ++dt) v[dt] = sb[L::VB + vrun * L::SUB + 32 * dt + lj];
-        if (tail) {
-          int lim = limit;
-          asm volatile("" : "+s"(lim));
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (16 * vrun + i >= lim) s[i] = -INFINITY;
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            const uint32_t keep = keep_mask<1>(lim - (16 * vrun + 4 * w));
-#pragma unroll
-            for (int dt = 0; dt < ND; ++dt) v[dt][w] &= keep;
-            e[w] &= keep;
-          }
-        }
-        st.template raise<16, 32>(s, scale);
-        st.weigh(s, scale);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] *= exponent_scale((e[i / 4] >> (8 * (i % 4))) & 0xffu);
-        const bf16x8 p0 = weights8(s), p1 = weights8(s + 8);
-        __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-        for (int dt = 0; dt < ND; ++dt) {
-          st.o[dt] = mfma(from_e4m3(v[dt][0], v[dt][1], 1.f), p0, st.o[dt]);
-          st.o[dt] = mfma(from_e4m3(v[dt][2], v[dt][3], 1.f), p1, st.o[dt]);
-        }
-        __builtin_amdgcn_s_setprio(0);
-      }
+      for (int i = 0; i < 16; ++i)
+        if (16 * (i / 8) + 8 * lh + i % 8 >= lim) s[i] = -INFINITY;
+      clear_tail(v, lim - 8 * lh);
     }
+    st.template raise<16, 32>(s, scale);
+    st.weigh(s, scale);
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const bf16x8 p = weights8(s + 8 * t);
+#pragma unroll
+      for (int dt = 0; dt < ND; ++dt) st.o[dt] = mfma(__builtin_bit_cast(bf16x8, v[dt]), p, st.o[dt]);
+      if (t) break;
+#pragma unroll
+      for (int dt = 0; dt < ND; ++dt) v[dt] = bf16_values(sb, dt, 1);
+      if (tail) clear_tail(v, limit - 16 - 8 * lh);
+    }
+    __builtin_amdgcn_s_setprio(0);
   }
 
   template <typename F>
@@ -1202,8 +1145,9 @@ hipError_t launch_tree(const TreeParams& p, int storage, int hd, hipStream_t s) 
 #define SP_TREE(HD_, E8_, ROWS_)                                                                   \
   if (hd == HD_ && e8 == E8_ && p.rows_per_wave == ROWS_)                                          \
     hipLaunchKernelGGL((tree_split<HD_, E8_, Wave##ROWS_>), grid, block, 0, s, p);
-    SP_TREE(128, false, 16) SP_TREE(128, false, 32) SP_TREE(128, true, 16) SP_TREE(128, true, 32)
-    SP_TREE(64, false, 16) SP_TREE(64, false, 32) SP_TREE(64, true, 16) SP_TREE(64, true, 32)
+      if (e8 && p.rows_per_wave != 16) return hipErrorInvalidValue;
+      SP_TREE(128, false, 16) SP_TREE(128, false, 32) SP_TREE(128, true, 16)
+      SP_TREE(64, false, 16) SP_TREE(64, false, 32) SP_TREE(64, true, 16)
 #undef SP_TREE
     }
     e = hipGetLastError();
