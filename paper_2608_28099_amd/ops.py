@@ -249,7 +249,7 @@ def cache_read(cache: PagedCache, seq_ids, positions, dtype=torch.bfloat16, k=No
             return cache_read(cache, seq_ids, positions, dtype, k, v, stream)
     if k is None and v is None:
         k = _empty((n, cache.n_kv_heads, hd), dtype, dev, stream)
-        v = _empty((n, cache.n_kv_heads, hd), dtype, dev, stream)
+        v = _empty_like(k, stream)
     else:
         dtype = k.dtype if k is not None else v.dtype
     if dtype not in _ROW_TYPES:
