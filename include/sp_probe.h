@@ -523,8 +523,9 @@ typedef struct sp_tree {
  * reach it, whatever it holds (NaN and infinities in masked nodes' keys and values, in
  * slots past a sequence's end).  The drafted keys and values are read from k and v and
  * never enter the cache (sp_probe_cache_write puts the accepted ones there).
- * Arithmetic: SP_BF16: bf16 products of the stored values (8-bit ones are exact in bf16),
- * the softmax's weights rounded to bf16 for the product with the values; fp32 sums,
+ * Arithmetic: SP_BF16: products of the stored values (8-bit ones are exact in bf16; with
+ * 8-bit keys, query values below 2^-14 of their row's largest, or below 2^-130, are rounded, by
+ * 2^-22 of that largest or 2^-136 at most), the softmax's weights rounded to bf16 for the product with the values; fp32 sums,
  * statistics and partial results.  SP_F32: fp32 throughout.  The result depends on the lengths
  * and shapes alone, not on the run (no atomics).
  *   seq_lens, block_table  as sp_probe_forward; a block id outside [0, num_blocks) is

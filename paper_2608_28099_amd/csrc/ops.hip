@@ -150,8 +150,8 @@ int64_t slots_of(int num_cus) { return (int64_t)num_cus * 3; }  // three workgro
 // rows on, where padding to 128 adds at most a fifth and pieces of kMinSplit tokens would still fill the device
 // twice.  Measured (in us, 16 rows a wave / 32): 64 sequences of 6000 tokens: 240 rows 607 / 523, 320 rows 756 / 665,
 // 480 rows 1113 / 937; 160 rows, padded to 192 or 256: 487 / 460; 16 of 4000, 160 rows: 76 / 86, 128 rows: 63 / 77;
-// 240 rows, 4 of 8000: 56.6 / 55.1, one of 2000: 20.2 / 23.6.  8-bit, 64 of 6000: 240 rows 626 / 652, 320 rows 794 / 873,
-// 480 rows 1189 / 1181, and two waves of 32 rows for every 64 (each half of a unit's tokens): 648, 811, 1212.
+// 240 rows, 4 of 8000: 56.6 / 55.1, one of 2000: 20.2 / 23.6.  8-bit, when keys were converted to bf16, 64 of 6000: 240
+// rows 626 / 652, 320 rows 794 / 873, 480 rows 1189 / 1181; now 577, 727 and 1086 in waves of 16.
 void row_groups(const sp_tree_config& c, int nodes, int num_cus, int* rows_per_wave, int* groups) {
   const int rows = nodes * (c.n_q_heads / c.n_kv_heads), g64 = (rows + 63) / 64, g128 = (rows + 127) / 128;
   const bool f32 = c.kv_dtype == SP_F32;
@@ -176,7 +176,8 @@ TreePlan tree_plan(const sp_tree_config& c, int nodes, int num_cus) {
   // As many splits as fill the device once, and pieces of at most an eighth of the longest sequence
   // (or 2048 tokens): a batch of long and short sequences takes several rounds, whose ends level
   // out (64 sequences of 2K-32K tokens, 320 rows: 1160-1176 us in splits of 4096-8192, 1432 of 1024,
-  // 1383 unsplit; 128 of 1K-8K 8-bit tokens, 64 rows: 218 us in splits of 2048, 236 of 1024, 256 unsplit).
+  // 1383 unsplit; 128 of 1K-8K 8-bit tokens, 64 rows: 208 us in splits of 2048; with keys
+  // converted to bf16 218 so, 236 in splits of 1024, 256 unsplit).
   // Then up to as many again, until the last round is full: of alike sequences a round that a third of
   // the device works on costs a whole one (32 of 131072 8-bit tokens, 4 rows: 1435 us in 4 splits
   // each, 1.33 rounds; 1327 in 8, 2.67; 1362 in 3, one; 2184 unsplit).

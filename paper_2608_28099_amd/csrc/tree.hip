@@ -11,8 +11,10 @@
 // lane receives of the first product are, as weights, its operand of the second.  For that the
 // keys' tokens go to the rows of the first product in an order of their own (Wave16, Wave32).
 // Units: 32 tokens of bf16 caches and nodes, 64 of 8-bit caches, 16 of fp32 (WaveF32), so that each reads 16 bytes
-// per lane at a time.  8-bit keys become bf16 with their exponent, exactly; the values'
-// exponents go to the weights instead, exactly too (a power of two).
+// per lane at a time.  8-bit keys meet the queries as they are, E4M3 with their exponents, in products of 128
+// dims: a bf16 query is two E4M3 values (split_queries), so that two products replace the keys' conversion
+// to bf16 (64 sequences of 6000 tokens, 320 rows: 794 -> 727 us).  8-bit values become bf16 bare, exactly; their exponents
+// go to the weights, exactly too (a power of two).
 #include <type_traits>
 
 #include "common.h"
@@ -60,6 +62,16 @@ __device__ __forceinline__ bf16x8 from_e4m3(uint32_t a, uint32_t b, float scale)
 }
 __device__ __forceinline__ float exponent_scale(uint32_t byte) {
   return __builtin_bit_cast(float, byte << 23);
+}
+
+__device__ __forceinline__ bool is_finite(float x) { return fabsf(x) <= 3.402823466e38f; }
+
+// C + A B of E4M3 values: lane l has of row (column) l % 16 the 16 values of k from 16 (l / 16) and the 16 from 64 + 16 (l / 16).
+// Powers of two 2^(e - 127): the lane's e scales the 32 values of k from 32 (l / 16).
+typedef uint32_t u32x8 __attribute__((ext_vector_type(8)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ f32x4 mfma16x16x128_e4m3(u32x8 a, u32x8 b, f32x4 c, int ea, int eb) {
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(__builtin_bit_cast(i32x8, a), __builtin_bit_cast(i32x8, b), c, 0, 0, 0, ea, 0, eb);
 }
 
 // Where they gain by it, waves raise their priority while they issue matrix products (s_setprio), so that of the
@@ -190,12 +202,68 @@ struct Wave16 {
   typedef Unit<HD, E8, PAD> U;
   RowState<NT, f32x4, 4> st;  // o[nt][r]: dim 16 nt + 4 la + r
   bf16x8 q[NC];
+  u32x8 qh, ql;       // 8-bit units: the lane's 32 dims of the row, q = qh 2^(eh - 127) + ql 2^(el - 127)
+  int eh, el;
   int li, la;
   __device__ __forceinline__ Wave16(int lane) : li(lane & 15), la(lane >> 4) { st.clear(); }
   __device__ __forceinline__ int row() const { return li; }
   __device__ __forceinline__ void load_queries(const bf16* p, bool vec) {
 #pragma unroll
     for (int c = 0; c < NC; ++c) q[c] = __builtin_bit_cast(bf16x8, row8(p + 8 * (la * NC + c), vec));
+  }
+
+  // Queries for the products with 8-bit keys: dims 32 la .. + 31 of the row (head dim 64: 16 la .. + 15, of which the
+  // second 16 bytes hold ql).  qh: E4M3 with the power of two that brings the row within 448; ql: what is left, times 16.
+  // Eight significant bits of bf16 are four and four, so the two are exact but for values below 2^-14 of the
+  // row's largest, which may be off by 2^-22 of that.
+  __device__ __forceinline__ void split_queries() {
+    u32x4 w[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) w[c] = __builtin_bit_cast(u32x4, q[c]);
+    uint32_t top = 0;  // the largest finite magnitude's bf16 bits
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t lo = w[c][i] & 0x7fffu, hi = (w[c][i] >> 16) & 0x7fffu;
+        top = max(top, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
+      }
+    top = max(top, (uint32_t)__shfl_xor((int)top, 16));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+    // 2^e with top <= 448 2^e = 1.75 2^(8 + e); e - 4 is kept within the scales' range
+    int e = (int)(top >> 7) - 135 + ((top & 0x7fu) > 0x60u ? 1 : 0);
+    e = e < -122 ? -122 : e;
+    const float f = __builtin_bit_cast(float, (uint32_t)(127 - e) << 23);
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; i += 2) {
+        int h = 0, l = 0;
+        float x[4], r[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t v = w[c][i + j / 2];
+          x[j] = __builtin_bit_cast(float, j & 1 ? v & 0xffff0000u : v << 16) * f;
+          x[j] = is_finite(x[j]) ? x[j] : __builtin_nanf("");
+        }
+        h = __builtin_amdgcn_cvt_pk_fp8_f32(x[0], x[1], h, false);
+        h = __builtin_amdgcn_cvt_pk_fp8_f32(x[2], x[3], h, true);
+        r[0] = 16.f * (x[0] - __builtin_amdgcn_cvt_f32_fp8(h, 0));
+        r[1] = 16.f * (x[1] - __builtin_amdgcn_cvt_f32_fp8(h, 1));
+        r[2] = 16.f * (x[2] - __builtin_amdgcn_cvt_f32_fp8(h, 2));
+        r[3] = 16.f * (x[3] - __builtin_amdgcn_cvt_f32_fp8(h, 3));
+        l = __builtin_amdgcn_cvt_pk_fp8_f32(r[0], r[1], l, false);
+        l = __builtin_amdgcn_cvt_pk_fp8_f32(r[2], r[3], l, true);
+        qh[2 * c + i / 2] = (uint32_t)h;
+        ql[2 * c + i / 2] = (uint32_t)l;
+      }
+    eh = e + 127;
+    el = e + 123;
+    if (HD == 64) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) qh[4 + i] = ql[i];
+      eh = la < 2 ? eh : el;
+    }
   }
 
   template <bool U8>
@@ -208,15 +276,14 @@ struct Wave16 {
     for (int h = 0; h < NH; ++h) d[h] = f32x4{0.f, 0.f, 0.f, 0.f};
     if constexpr (U8) {
       const u32x4 ek = sb[L::EB + 2 * run];
+      constexpr int PL = HD / 64;  // pieces of a lane
 #pragma unroll
       for (int h = 0; h < NH; ++h) {
-        const float f = exponent_scale((ek[h] >> (8 * (li & 3))) & 0xffu);
-#pragma unroll
-        for (int c = 0; c < NC / 2; ++c) {
-          const u32x4 w = sb[run * L::KP + (la * (NC / 2) + c) * 16 + first + 4 * h];
-          d[h] = mfma16x16x32_bf16(from_e4m3(w[0], w[1], f), q[2 * c], d[h]);
-          d[h] = mfma16x16x32_bf16(from_e4m3(w[2], w[3], f), q[2 * c + 1], d[h]);
-        }
+        const u32x4* at = &sb[run * L::KP + la * PL * 16 + first + 4 * h];
+        const u32x8 k = __builtin_shufflevector(at[0], at[16 * (PL - 1)], 0, 1, 2, 3, 4, 5, 6, 7);
+        const int e = (int)((ek[h] >> (8 * (li & 3))) & 0xffu);
+        d[h] = mfma16x16x128_e4m3(k, qh, d[h], e, eh);
+        if (HD == 128) d[h] = mfma16x16x128_e4m3(k, ql, d[h], e, el);
       }
     } else {
 #pragma unroll
@@ -553,8 +620,6 @@ struct WaveF32 {
   }
 };
 
-__device__ __forceinline__ bool is_finite(float x) { return fabsf(x) <= 3.402823466e38f; }
-
 // Nodes 32 u .. of n into the LDS image of a bf16 unit, by the whole workgroup.  Values that
 // are not finite become 0 there (0 * NaN would carry a hidden node's values into every row);
 // returns whether this lane met one.
@@ -681,9 +746,9 @@ __device__ __forceinline__ float lse_of(float m, float l) {
 // for tree_merge.
 // What bounds it (8 KV heads, head dim 128).  fp32, the matrix cores: 32 sequences of 8000 tokens, 240 rows: 2060 us, 122
 // TFLOP/s of 157 at the nominal clock; 4 rows, the read: 349 us, 6.0 TB/s.  Few rows, the read: 32 sequences of 131072 8-bit tokens, 4 rows each:
-// 1335 us for 8.7 GB, 6.5 TB/s, where plain reads reach 7.1.  64 rows of 8-bit tokens: the conversions,
-// one per two values and wave, beside both products and the exponentials: 128 sequences of 1K-8K: 220 us, 4.0
-// TB/s and 485 TFLOP/s, matrix cores 27% busy.  320 rows of bf16: 64 sequences of 2K-32K: 1165 us with their join, 830
+// 1330 us for 8.7 GB, 6.5 TB/s, where plain reads reach 7.1.  64 rows of 8-bit tokens: vector issue, most of it the
+// values' conversions, one per two values and wave, and the exponentials: 128 sequences of 1K-8K: 208 us, 4.2
+// TB/s and 513 TFLOP/s.  320 rows of bf16: 64 sequences of 2K-32K: 1165 us with their join, 830
 // TFLOP/s (a large library product: 1300), matrix cores 55% busy, three waves per SIMD by registers and LDS; a sixth
 // of its wave slots have no rows (320 in groups of 128).  One sequence of 2048, 240 rows: 20 us, a chain of loads.
 constexpr int kWaves = 4;
@@ -845,6 +910,7 @@ __global__ __launch_bounds__(64 * kWaves, 3) void tree_split(const TreeParams p)
         });
       });
     }
+  if constexpr (E8) wv.split_queries();
   int buf = 0;
   for (int u = 0; u < nunits; ++u) {
     // this wave's loads of unit u have landed; after the barrier everyone's have, and all are past

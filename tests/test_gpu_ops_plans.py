@@ -360,3 +360,36 @@ def test_refusals_of_tensors(dev):
     for kw in (dict(max_seq_len=c.cache.capacity + 1), dict(max_seq_len=-1), dict(workspace=torch.zeros(16, dtype=torch.uint8, device=dev))):
         with pytest.raises(binding.ProbeError):
             ops.tree_attention(c.cache, c.seq_lens, q, k, v, **kw)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("power", [0, 100, -100])
+def test_queries_of_wide_range_over_8_bit_keys(dev, hd, power):
+    """Queries from 2^-40 to 4 in a row, rows of zeros, of one value, and whole calls times a large or small power of two
+    (and the scale over it)."""
+    from oracle import cacheops as oracle
+    from tests.test_gpu_ops import dense
+    lens, t, nq, nkv = (130, 700), 9, 4, 2
+    c = Tree(dev, torch.float8_e4m3fn, lens, t, nq, nkv, hd, 16, seed=73)
+    gen = seeded(74)
+    x = c.x.float()
+    small = torch.exp2(-40 * torch.rand(x[:, :, :nq].shape, generator=gen))
+    x[:, 1:5, :nq] *= small[:, 1:5]
+    x[:, 5, :nq] = 0
+    x[:, 6, :nq] = 0
+    x[:, 6, :nq, 7] = 3.0
+    x = (x * 3).bfloat16()
+    scale = hd ** -0.5
+    q, k, v = c.qkv(x)
+    got = ops.tree_attention(c.cache, c.seq_lens, q * 2.0 ** power, k, v, mask=words_of(c.see).to(dev), max_seq_len=700,
+                             scale=scale * 2.0 ** -power).cpu()
+    for b, n in enumerate(lens):
+        kc, vc = dense(c.cache, b, n)
+        q, k, v = x[b, :, :nq], x[b, :, nq:nq + nkv], x[b, :, nq + nkv:]
+        ref, _, mag, big = oracle.tree_attention(q, kc, vc, k, v, c.see[b], scale)
+        # Tree.check's terms, and each query value off by 2^-22 of its row's largest
+        far = scale * 2.0 ** -22 * q.double().abs().amax(-1, keepdim=True) * kc.double().abs().sum(-1).max()
+        eps = 2 * (hd * 2.0 ** -24 * big + 2.0 ** -22) + 2 * (n + t + 8) * 2.0 ** -24
+        eps = eps + 2 * (far if torch.as_tensor(big).dim() == 3 else far.max())
+        tol = mag * (2.0 ** -8 + eps) * (1 + 2.0 ** -6) + 2.0 ** -8 * ref.abs() + 1e-30
+        assert torch.all((got[b].double() - ref).abs() <= tol), float(((got[b].double() - ref).abs() / tol).max())
