@@ -133,6 +133,8 @@ def rotary(rot, positions, q, k=None, out=None, k_out=None, transpose=False, str
     hd, dev, dtype, n = rot.head_dim, q.device, q.dtype, q.shape[0]
     if dtype not in _ROW_TYPES:
         raise ValueError("q must be float32 or bfloat16")
+    if q.dim() != 3 or (k is not None and k.dim() != 3):  # (_rows knows the nodes of a batch too)
+        raise ValueError("q and k must be [rows, heads, head_dim]")
     if _elsewhere(dev):
         with torch.cuda.device(dev):
             return rotary(rot, positions, q, k, out, k_out, transpose, stream)
@@ -244,6 +246,8 @@ def cache_read(cache: PagedCache, seq_ids, positions, dtype=torch.bfloat16, k=No
     dtype; given k and v (either or both) are written instead: rows with ids or positions out
     of range are left as they are."""
     dev, n, hd = cache.device, seq_ids.shape[0], cache.head_dim
+    if (k is not None and k.dim() != 3) or (v is not None and v.dim() != 3):
+        raise ValueError("k and v must be [rows, heads, head_dim]")
     if _elsewhere(dev):
         with torch.cuda.device(dev):
             return cache_read(cache, seq_ids, positions, dtype, k, v, stream)
