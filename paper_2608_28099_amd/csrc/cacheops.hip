@@ -133,7 +133,8 @@ __global__ __launch_bounds__(256) void rotary_rows(const RotaryParams p) {
   typedef T Piece __attribute__((ext_vector_type(V)));
   __shared__ __align__(16) float cs[R][64], sn[R][64];
   __shared__ int live[R];
-  const int row0 = blockIdx.x * R, hd = p.rot.head_dim, rd = p.rot.rotary_dim, half = rd >> 1;
+  const int row0 = (blockIdx.x + gridDim.x * blockIdx.y) * R, hd = p.rot.head_dim, rd = p.rot.rotary_dim, half = rd >> 1;
+  if (row0 >= p.n_rows) return;
   if ((int)threadIdx.x < R) live[threadIdx.x] = row0 + (int)threadIdx.x < p.n_rows && p.positions[row0 + threadIdx.x] >= 0;
   for (int e = threadIdx.x; e < R * half; e += 256) {
     const int r = e / half, i = e - r * half;
@@ -606,16 +607,19 @@ int heads_per_wg(const CacheParams& p, int n_cus) {
 template <typename T>
 hipError_t rotary_typed(const RotaryParams& p, int n_cus, hipStream_t s) {
   constexpr int V = 16 / sizeof(T);
-  const dim3 grid(p.n_rows), block(256);
+  // a dimension of a launch has less than 2^32 threads: groups of rows past kAcross go on in the grid's second one
+  constexpr int kAcross = 1 << 23;
+  auto grid = [](int groups) { return dim3(groups < kAcross ? groups : kAcross, (groups + kAcross - 1) / kAcross); };
+  const dim3 block(256);
   if (p.vec && p.rot.layout == SP_ROTARY_INTERLEAVED) {
     constexpr int R = 4;
     if (p.n_rows >= 4 * R * n_cus)
-      hipLaunchKernelGGL((rotary_rows<T, kInterleaved, R>), dim3((p.n_rows + R - 1) / R), block, 0, s, p);
-    else hipLaunchKernelGGL((rotary_rows<T, kInterleaved, 1>), grid, block, 0, s, p);
+      hipLaunchKernelGGL((rotary_rows<T, kInterleaved, R>), grid((p.n_rows + R - 1) / R), block, 0, s, p);
+    else hipLaunchKernelGGL((rotary_rows<T, kInterleaved, 1>), grid(p.n_rows), block, 0, s, p);
   } else if (p.vec && p.rot.rotary_dim % (2 * V) == 0) {
-    hipLaunchKernelGGL((rotary_rows<T, kHalf, 1>), grid, block, 0, s, p);
+    hipLaunchKernelGGL((rotary_rows<T, kHalf, 1>), grid(p.n_rows), block, 0, s, p);
   } else {
-    hipLaunchKernelGGL((rotary_rows<T, kScalar, 1>), grid, block, 0, s, p);
+    hipLaunchKernelGGL((rotary_rows<T, kScalar, 1>), grid(p.n_rows), block, 0, s, p);
   }
   return hipGetLastError();
 }

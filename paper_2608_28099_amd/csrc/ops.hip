@@ -21,7 +21,8 @@ bool is_pow2(int64_t x) { return x > 0 && (x & (x - 1)) == 0; }
 int ilog2(int64_t x) { int r = 0; while ((int64_t(1) << r) < x) ++r; return r; }
 int size_of(int dtype) { return dtype == SP_F32 ? 4 : dtype == SP_BF16 ? 2 : 1; }
 
-// Rows of a call: a launch has less than 2^32 threads along x, and a rotation takes 64 per row.
+// Rows of a call.  The cache's kernels take 4 threads per row along the grid's first dimension (less than 2^32 fit); rotations,
+// with up to 256 per row, go on along its second.
 constexpr int kMaxRows = (1 << 26) - 1;
 
 // The current device: whether the kernels run on it, and its compute units (asked once).
