@@ -84,6 +84,9 @@ __device__ __forceinline__ f32x4 mfma16x16x128_e4m3(u32x8 a, u32x8 b, f32x4 c, i
 // across lanes and the rescaling of O.
 constexpr float kRescaleLog2 = 8.0f;
 
+// The reference maximum of a row that has met no score yet: the lowest finite value, below which no finite score lies.
+constexpr float kLowest = -3.402823466e38f;
+
 // LDS image of a unit, in 16-byte pieces: NSUB runs of 16 tokens (each inside one
 // block), their keys, then their values.  A run's keys: piece c * 16 + t = 16 bytes of dims
 // of token t; its values: 8-bit: piece d = dim d of its 16 tokens; bf16: piece
@@ -155,7 +158,7 @@ struct RowState {
     for (int j = 0; j < NO; ++j)
 #pragma unroll
       for (int r = 0; r < OV; ++r) o[j][r] = 0.f;
-    m = kNegBig;
+    m = kLowest;
     l = 0.f;
   }
   // Moves the reference maximum (and l and O) where one of the lane's scores s (products not yet scaled,
@@ -965,7 +968,7 @@ __global__ __launch_bounds__(256) void tree_merge(const TreeParams p) {
   const int ns = (len + p.split_len - 1) / p.split_len;
   const int r = tid & 15, c = tid >> 4;
   const float2* ml = p.ml_part + 16 * tile_of(p, b, g, 0, row0) + r;
-  float m = kNegBig, l = 0.f;
+  float m = kLowest, l = 0.f;
   for (int s = c; s < ns; s += 16) m = fmaxf(m, ml[(int64_t)s * p.r_alloc].x);
   red[r][c] = m;
   __syncthreads();
@@ -1066,7 +1069,7 @@ __global__ __launch_bounds__(64 * kF32Waves) void tree_split_f32(const TreeParam
     for (int e = 0; e < 4; ++e) q[j][e] = qr[16 * j + 4 * la + e];
     o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  float m = kNegBig, l = 0.f;
+  float m = kLowest, l = 0.f;
   // scores and values (zero where masked and not finite) of 16 tokens
   auto step = [&](f32x4 (&k)[NJ], f32x4 (&v)[NJ], uint32_t seen) __attribute__((always_inline)) {
     f32x4 sc = f32x4{0.f, 0.f, 0.f, 0.f}, sc2 = sc;

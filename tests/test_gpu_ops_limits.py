@@ -1,12 +1,14 @@
 """The cache operators at the ends of what they take."""
 from __future__ import annotations
 
+import math
+
 import pytest
 import torch
 
 from oracle import cacheops as oracle
 from paper_2608_28099_amd import binding, ops
-from tests.test_gpu_ops import rotation_error
+from tests.test_gpu_ops import STORES, make_cache, rotation_error, seeded, tokens
 
 pytestmark = pytest.mark.gpu
 
@@ -41,3 +43,78 @@ def test_rotary_of_the_most_rows(dev, layout, dim, n):
     got = x[-300:].cpu()
     assert rotation_error(got[live], last[live], want[live], theta, scale, layout, last_pos[live]) <= 1
     assert torch.equal(got[~live], last[~live])
+
+
+class Ladder:
+    """A call whose scores are sign * c * 2^power times the scale, exactly until the scale: queries are
+    2^(power / 2) in one dim, keys c * sign times the rest there, c a whole number.  One token of every sequence, cached
+    or the first node, has the best c, by 1 at least: the others' weights vanish, so the row is that token's value."""
+
+    def __init__(self, dev, store, lens, nodes, group, hd, sign, power, best, bound=None):
+        gen = seeded(nodes + power)
+        nkv, dim = 2, 5
+        self.dtype = torch.float32 if store == torch.float32 else torch.bfloat16
+        nq = nkv * group
+        self.cache = make_cache(dev, store, lens, nkv, hd, 16, seed=4, fill=math.nan)
+        if bound is not None:  # a table (and so a plan) of longer sequences
+            t = self.cache.block_table
+            t = torch.cat([t, t[:, -1:].expand(-1, -(-bound // 16) - t.shape[1])], 1).contiguous()
+            self.cache = ops.PagedCache(self.cache.k, self.cache.v, 16, t, self.cache.k_exponents, self.cache.v_exponents)
+        seq, pos = tokens(lens)
+        c = torch.randint(2, 4, (len(seq),), generator=gen).double()
+        cn = torch.randint(2, 4, (len(lens), nodes), generator=gen).double()
+        top = 1.0 if sign < 0 else 4.0
+        winner = torch.tensor([2 * n // 3 for n in lens])
+        first = torch.tensor([sum(lens[:b]) for b in range(len(lens))])
+        if best == "cached":
+            c[first + winner] = top
+        else:
+            cn[:, 0] = top
+        kv = torch.randn((len(seq), 2 * nkv, hd), generator=gen).double()
+        kv[:, :nkv] = 0
+        kv[:, :nkv, dim] = (sign * c * 2.0 ** (power - power // 2))[:, None]
+        kv = kv.to(self.dtype).to(dev)
+        ops.cache_write(self.cache, seq.to(dev), pos.to(dev), kv[:, :nkv], kv[:, nkv:])
+        q = torch.zeros((len(lens), nodes, nq, hd), dtype=torch.float64)
+        q[..., dim] = 2.0 ** (power // 2)
+        k = torch.zeros((len(lens), nodes, nkv, hd), dtype=torch.float64)
+        k[..., dim] = (sign * cn * 2.0 ** (power - power // 2))[..., None]
+        v = torch.randn((len(lens), nodes, nkv, hd), generator=gen)
+        self.q, self.k, self.v = (x.to(self.dtype).to(dev) for x in (q, k, v))
+        if best == "cached":
+            value = ops.cache_read(self.cache, torch.arange(len(lens), dtype=torch.int32, device=dev),
+                                   winner.int().to(dev), torch.float32)[1].cpu()
+        else:
+            value = self.v[:, 0].float().cpu()
+        self.value = value[:, None, :, None].expand(-1, nodes, -1, group, -1).reshape(len(lens), nodes, nq, hd).double()
+        self.score = sign * top * 2.0 ** power
+        self.seq_lens = torch.tensor(lens, dtype=torch.int32, device=dev)
+        self.bound = max(lens) if bound is None else bound
+
+    def check(self, scale):
+        lse = torch.zeros(self.q.shape[:3], device=self.q.device)
+        out = ops.tree_attention(self.cache, self.seq_lens, self.q, self.k, self.v, lse=lse, scale=scale,
+                                 max_seq_len=self.bound).cpu().double()
+        # one weight, within a factor of 2^8 of 1: rounded (bf16), its product and the sum over it; the result's rounding
+        u = 0.0 if self.dtype == torch.float32 else 2.0 ** -8
+        tol = (2 * u + 2.0 ** -21) * self.value.abs()
+        assert torch.isfinite(out).all(), "not finite"
+        assert torch.all((out - self.value).abs() <= tol), float(((out - self.value).abs() - tol).max())
+        # the scale and its product with log2(e), the score, the maximum times ln(2): half a step each, two spare
+        want = self.score * scale
+        assert torch.all((lse.cpu().double() - want).abs() <= 6 * 2.0 ** -24 * abs(want) + 2.0 ** -20), (float(lse.flatten()[0]), want)
+
+
+# sequences, nodes, query heads per KV head, the bound that plans the call: one split and several; fp32 by eight waves
+# and staged; waves of 16 rows and, from 129 rows with much to do, of 32
+LADDERS = [((40, 7), 3, 1, None), ((3000, 700), 5, 4, None), ((300, 90), 40, 5, None), ((300, 90), 40, 5, 131072)]
+
+
+@pytest.mark.parametrize("store", STORES)
+@pytest.mark.parametrize("lens,nodes,group,bound", LADDERS)
+@pytest.mark.parametrize("best", ["cached", "node"])
+@pytest.mark.parametrize("power", [101, 120])
+def test_scores_far_below_zero(dev, store, lens, nodes, group, bound, best, power):
+    """Rows all of whose scores are below -1e30 see their tokens all the same.  (The scale is ln 2, which leaves whole
+    scores in the kernels' units.)"""
+    Ladder(dev, store, lens, nodes, group, 64, -1, power, best, bound).check(math.log(2.0))
