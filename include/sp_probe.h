@@ -526,7 +526,10 @@ typedef struct sp_tree {
  * Arithmetic: SP_BF16: products of the stored values (8-bit ones are exact in bf16; with
  * 8-bit keys, query values below 2^-14 of their row's largest, or below 2^-130, are rounded, by
  * 2^-22 of that largest or 2^-136 at most), the softmax's weights rounded to bf16 for the product with the values; fp32 sums,
- * statistics and partial results.  SP_F32: fp32 throughout.  The result depends on the lengths
+ * statistics and partial results.  SP_F32: fp32 throughout.  A score (times log2(e)) past fp32's range is an
+ * infinity; a row that sees scores of -infinity alone counts as one that sees nothing.  Weights times values are
+ * summed before they are divided by the weights' sum, with weights up to 2^8: magnitudes above 2^119 / tokens may
+ * overflow there.  The result depends on the lengths
  * and shapes alone, not on the run (no atomics).
  *   seq_lens, block_table  as sp_probe_forward; a block id outside [0, num_blocks) is
  *              read as block 0 (no fault, that sequence's result means nothing)

@@ -87,6 +87,13 @@ constexpr float kRescaleLog2 = 8.0f;
 // The reference maximum of a row that has met no score yet: the lowest finite value, below which no finite score lies.
 constexpr float kLowest = -3.402823466e38f;
 
+// The weight's exponent s scale - m is one fma, exact but for its own rounding, while m is the product of the largest s rounded by
+// itself: they differ by up to half a step of m, a power of two that all of the row's weights share and the division by their
+// sum takes out.  Of maxima beyond kFineLog2 half a step is 1 and more, soon past the exponent's range, so there the difference
+// is kept (RowState::rest) and taken off.  The test in every unit costs 1-2% (64 sequences of 2K-32K tokens, 320 rows, bf16:
+// 1184 -> 1208 us; 64 of 6000, 320 rows, 8-bit: 712 -> 722).
+constexpr float kFineLog2 = 16777216.0f;
+
 // LDS image of a unit, in 16-byte pieces: NSUB runs of 16 tokens (each inside one
 // block), their keys, then their values.  A run's keys: piece c * 16 + t = 16 bytes of dims
 // of token t; its values: 8-bit: piece d = dim d of its 16 tokens; bf16: piece
@@ -153,6 +160,7 @@ template <int NO, typename OVec, int OV>
 struct RowState {
   OVec o[NO];
   float m, l;
+  float rest;  // largest score times scale - m, where that is taken off (else 0)
   __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int j = 0; j < NO; ++j)
@@ -160,6 +168,7 @@ struct RowState {
       for (int r = 0; r < OV; ++r) o[j][r] = 0.f;
     m = kLowest;
     l = 0.f;
+    rest = 0.f;
   }
   // Moves the reference maximum (and l and O) where one of the lane's scores s (products not yet scaled,
   // masked ones -inf) exceeds it by too much.  FROM: the first lane bit that tells lanes of a row apart.
@@ -168,11 +177,12 @@ struct RowState {
     float mx = fmaxf(s[0], s[1]);
 #pragma unroll
     for (int i = 2; i < S; ++i) mx = fmaxf(mx, s[i]);
-    mx *= scale;
-    if (__any(mx > m + kRescaleLog2)) {
+    if (__any(mx * scale > m + kRescaleLog2)) {
 #pragma unroll
       for (int b = FROM; b < 64; b <<= 1) mx = fmaxf(mx, __shfl_xor(mx, b));
-      mx = fmaxf(mx, m);
+      const float top = mx * scale;
+      if (top > m) rest = fabsf(top) > kFineLog2 ? fmaf(mx, scale, -top) : 0.f;
+      mx = fmaxf(top, m);
       const float alpha = fast_exp2(m - mx);
       m = mx;
       l *= alpha;
@@ -186,8 +196,13 @@ struct RowState {
   template <int S>
   __device__ __forceinline__ void weigh(float (&s)[S], float scale) {
 #pragma unroll
+    for (int i = 0; i < S; ++i) s[i] = fmaf(s[i], scale, -m);
+    if (__any(rest != 0.f))
+#pragma unroll
+      for (int i = 0; i < S; ++i) s[i] -= rest;
+#pragma unroll
     for (int i = 0; i < S; ++i) {
-      s[i] = fast_exp2(fmaf(s[i], scale, -m));
+      s[i] = fast_exp2(s[i]);
       l += s[i];
     }
   }
@@ -825,18 +840,19 @@ __global__ __launch_bounds__(64 * kWaves, 3) void tree_split(const TreeParams p)
   };
   // This wave's run of a unit, and what it loads of it: first kind 0 keys, 1 values.
   const int run = wave * NSUB / W, kind0 = KIND == 1 ? wave & 1 : 0, part = L::PARTS == 1 ? 0 : wave >> 1;
-  uint32_t lane_off[KIND][IPG];
+  uint32_t lane_off[KIND];  // of the first load's pieces; the next 64 lie 64 bs bytes on (an offset for each load takes registers
+                            // that waves of 32 rows lack: 1208 -> 1385 us as above)
   const char* kind_base[KIND];  // a run's place: kind_base + block * block_step + (slot << slot_shift)
   uint64_t block_step[KIND];
   int slot_shift[KIND], piece0[KIND];
   // Loads are streaming (read once by this launch), unless another query group reads the
   // same blocks, or a unit takes less than 64 bytes of a dim's row of values.
   bool stream[KIND];
+  const int64_t step64 = (int64_t)64 << c.bs_log2;
 #pragma unroll
   for (int k = 0; k < KIND; ++k) {
     const bool v = kind0 + k;
-#pragma unroll
-    for (int j = 0; j < IPG; ++j) lane_off[k][j] = v ? L::value_off(64 * (IPG * part + j) + lane, bs) : L::key_off(64 * (IPG * part + j) + lane, bs);
+    lane_off[k] = v ? L::value_off(64 * IPG * part + lane, bs) : L::key_off(64 * IPG * part + lane, bs);
     kind_base[k] = v ? (const char*)c.v + g * c.v_sh * ESZ : (const char*)c.k + g * c.k_sh * ESZ;
     block_step[k] = (uint64_t)(v ? c.v_sb : c.k_sb) * ESZ;
     slot_shift[k] = v ? (E8 ? 0 : F32 ? 2 : 1) : 4;
@@ -872,10 +888,10 @@ __global__ __launch_bounds__(64 * kWaves, 3) void tree_split(const TreeParams p)
       u32x4* to = &stage[buf][piece0[k]];
       if (stream[k]) {
 #pragma unroll
-        for (int j = 0; j < IPG; ++j) ld16_to_lds(base, lane_off[k][j], to + 64 * j);
+        for (int j = 0; j < IPG; ++j) ld16_to_lds(base + j * step64, lane_off[k], to + 64 * j);
       } else {
 #pragma unroll
-        for (int j = 0; j < IPG; ++j) ld16_to_lds<false>(base, lane_off[k][j], to + 64 * j);
+        for (int j = 0; j < IPG; ++j) ld16_to_lds<false>(base + j * step64, lane_off[k], to + 64 * j);
       }
     }
     if constexpr (E8)

@@ -118,3 +118,13 @@ def test_scores_far_below_zero(dev, store, lens, nodes, group, bound, best, powe
     """Rows all of whose scores are below -1e30 see their tokens all the same.  (The scale is ln 2, which leaves whole
     scores in the kernels' units.)"""
     Ladder(dev, store, lens, nodes, group, 64, -1, power, best, bound).check(math.log(2.0))
+
+
+@pytest.mark.parametrize("store", STORES)
+@pytest.mark.parametrize("lens,nodes,group,bound", LADDERS)
+@pytest.mark.parametrize("best", ["cached", "node"])
+@pytest.mark.parametrize("sign,power", [(1, 26), (-1, 26), (1, 31), (-1, 33), (1, 36), (-1, 45), (1, 100), (-1, 118)])
+def test_scores_whose_steps_are_large(dev, store, lens, nodes, group, bound, best, sign, power):
+    """Scores so large that one step of fp32 between them is many powers of two of the weights."""
+    for scale in (0.125, 0.3):
+        Ladder(dev, store, lens, nodes, group, 64, sign, power, best, bound).check(scale)
