@@ -923,9 +923,10 @@ __global__ __launch_bounds__(64 * kWaves, 3) void tree_split(const TreeParams p)
       // the values that are not finite, kept out of the products, reach the rows that see them alone
       wv.node_unit(stage[D], seen, p.scale_log2, odd, [&](int t, float w) {
         if (NODES * u + t >= n) return;
+        const bool sees = (seen >> t) & 1;  // (a weight may have vanished: 0 times infinity is NaN, as of cached tokens)
         wv.add4([&](int d, float o) {
           const float x = to_f32(vb[(int64_t)(NODES * u + t) * p.v.row + d]);
-          return w != 0.f && !is_finite(x) ? fmaf(w, x, o) : o;
+          return sees && !is_finite(x) ? fmaf(w, x, o) : o;
         });
       });
     }
@@ -1170,7 +1171,7 @@ __global__ __launch_bounds__(64 * kF32Waves) void tree_split_f32(const TreeParam
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const float x = vb[(int64_t)(t0 + t) * p.v.row + 16 * j + 4 * la + r];
-            if (w != 0.f && !(fabsf(x) <= 3.402823466e38f)) o[j][r] = fmaf(w, x, o[j][r]);
+            if (((seen >> t) & 1) && !is_finite(x)) o[j][r] = fmaf(w, x, o[j][r]);
           }
       }
     }

@@ -8,7 +8,7 @@ import torch
 
 from oracle import cacheops as oracle
 from paper_2608_28099_amd import binding, ops
-from tests.test_gpu_ops import STORES, make_cache, rotation_error, seeded, tokens
+from tests.test_gpu_ops import STORES, Tree, make_cache, rotation_error, seeded, tokens, words_of
 
 pytestmark = pytest.mark.gpu
 
@@ -128,3 +128,27 @@ def test_scores_whose_steps_are_large(dev, store, lens, nodes, group, bound, bes
     """Scores so large that one step of fp32 between them is many powers of two of the weights."""
     for scale in (0.125, 0.3):
         Ladder(dev, store, lens, nodes, group, 64, sign, power, best, bound).check(scale)
+
+
+@pytest.mark.parametrize("store", STORES)
+@pytest.mark.parametrize("lens,group,bound", [((50, 0), 2, None), ((300, 90), 5, None), ((300, 90), 5, 131072)])
+@pytest.mark.parametrize("poison", [math.nan, math.inf, -math.inf])
+def test_values_that_are_not_finite_under_weights_that_vanish(dev, store, lens, group, bound, poison):
+    """A node's value reaches every row that sees it, as a cached one does, also where its weight is too small
+    for fp32 (0 times infinity or NaN is NaN); rows that do not see it stay as they are."""
+    t, nq, nkv, hd = 40, 2 * group, 2, 64
+    c = Tree(dev, store, lens, t, nq, nkv, hd, 16, seed=22)
+    if bound is not None:
+        table = c.cache.block_table
+        table = torch.cat([table, table[:, -1:].expand(-1, -(-bound // 16) - table.shape[1])], 1).contiguous()
+        c.cache = ops.PagedCache(c.cache.k, c.cache.v, 16, table, c.cache.k_exponents, c.cache.v_exponents)
+    see = torch.eye(t).bool().expand(len(lens), t, t).clone()
+    see[:, 20:, 7] = True
+    x = c.x.clone()
+    x[:, :, :nq, 0] = 64.0                                # node 7's scores: near -64 * 512 / 8 in the rows that see it
+    x[:, 7, nq:nq + nkv, 0] = -512.0
+    x[:, 7, nq + nkv:] = poison
+    q, k, v = c.qkv(x)
+    out = ops.tree_attention(c.cache, c.seq_lens, q, k, v, mask=words_of(see).to(dev), max_seq_len=bound or max(lens)).cpu()
+    assert not torch.isfinite(out[:, 20:].float()).any()
+    assert torch.isfinite(out[:, :7].float()).all() and torch.isfinite(out[:, 8:20].float()).all()
