@@ -496,7 +496,7 @@ typedef struct sp_tree_config {
   int32_t max_nodes;              /* 1..256 */
   int32_t max_batch;              /* the launch is planned for it and max_seq_len: near a call's own, best */
   int32_t max_seq_len;            /* longest context a call may pass, up to 2^30; lengths are clamped to [0, max_seq_len] */
-  float scale;                    /* factor on the scores; 0: 1 / sqrt(head_dim) */
+  float scale;                    /* factor on the scores, up to fp32's largest value over log2(e); 0: 1 / sqrt(head_dim) */
   int32_t reserved;               /* 0 */
 } sp_tree_config;
 

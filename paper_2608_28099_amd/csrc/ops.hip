@@ -115,13 +115,15 @@ StoreArg store_arg(const sp_kv_store* s, const int32_t* block_table) {
   return a;
 }
 
+constexpr double kLog2e = 1.4426950408889634;
+
 int check_tree_config(const sp_tree_config* c) {
   if (!c || c->reserved) return SP_ERR_INVALID_ARG;
   if (c->n_q_heads < 1 || c->n_kv_heads < 1 || c->n_q_heads % c->n_kv_heads) return SP_ERR_INVALID_ARG;
   if (c->dtype != SP_F32 && c->dtype != SP_BF16) return SP_ERR_INVALID_ARG;
   if (c->kv_dtype != SP_F32 && c->kv_dtype != SP_BF16 && c->kv_dtype != SP_E4M3) return SP_ERR_INVALID_ARG;
   if (c->max_nodes < 1 || c->max_batch < 1 || c->max_seq_len < 0) return SP_ERR_INVALID_ARG;
-  if (!(c->scale >= 0.f) || !std::isfinite(c->scale)) return SP_ERR_INVALID_ARG;
+  if (!(c->scale >= 0.f) || !std::isfinite((float)(c->scale * kLog2e))) return SP_ERR_INVALID_ARG;
   if (c->head_dim != 64 && c->head_dim != 128) return SP_ERR_UNSUPPORTED;
   if ((c->dtype == SP_F32) != (c->kv_dtype == SP_F32)) return SP_ERR_UNSUPPORTED;
   if (c->max_nodes > 256 || c->n_q_heads > 4096 || c->max_batch > 65535 || c->max_seq_len > 1 << 30) return SP_ERR_UNSUPPORTED;
@@ -448,6 +450,6 @@ SP_API int sp_probe_tree_attention(const sp_tree_config* c, const sp_kv_store* s
   p.group = c->n_q_heads / c->n_kv_heads;
   p.max_seq_len = c->max_seq_len;
   const double scale = c->scale > 0.f ? (double)c->scale : 1.0 / std::sqrt((double)c->head_dim);
-  p.scale_log2 = (float)(scale * 1.4426950408889634);
+  p.scale_log2 = (float)(scale * kLog2e);
   return launch_tree(p, c->kv_dtype, c->head_dim, (hipStream_t)stream) == hipSuccess ? SP_OK : SP_ERR_HIP;
 }

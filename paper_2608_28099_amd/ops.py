@@ -314,8 +314,10 @@ def tree_attention(cache: PagedCache, seq_lens, q, k, v, mask=None, counts=None,
         max_seq_len = cache.capacity
     if scale is None:
         scale = 0.0
-    elif not (math.isfinite(scale) and scale > 0):
-        raise ValueError("scale must be positive")
+    else:
+        scale = ctypes.c_float(scale).value  # what the library receives; its 0 means the default
+        if not (math.isfinite(scale) and scale > 0):
+            raise ValueError("scale must be positive and within float32's range")
     if _elsewhere(dev):
         with torch.cuda.device(dev):
             return tree_attention(cache, seq_lens, q, k, v, mask, counts, max_seq_len, scale or None, out, lse, workspace,

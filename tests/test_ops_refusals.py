@@ -1,6 +1,8 @@
 """Calls of the cache operators that are refused before anything reaches a device (CPU only)."""
 from __future__ import annotations
 
+import ctypes
+import math
 import os
 
 import pytest
@@ -25,3 +27,19 @@ def test_rows_of_a_batch_of_trees():
                  lambda: ops.cache_read(cache, ids, ids, v=x), lambda: ops.cache_read(cache, ids, ids, k=x, v=flat)):
         with pytest.raises(ValueError, match=shape):
             call()
+
+
+def test_scales_that_fp32_does_not_hold():
+    """A positive scale that fp32 rounds to 0 would ask for the default one."""
+    k = torch.zeros(4, 2, 2048, dtype=torch.bfloat16)
+    cache = ops.PagedCache(k, k, 16, torch.zeros(1, 2, dtype=torch.int32))
+    x = torch.zeros(1, 3, 2, 128, dtype=torch.bfloat16)
+    for scale in (1e-46, 1e-60, 1e39, 1e300, 0.0, -0.5, math.inf, math.nan):
+        with pytest.raises(ValueError, match="scale"):
+            ops.tree_attention(cache, torch.zeros(1, dtype=torch.int32), x, x, x, scale=scale)
+    cfg = binding.sp_tree_config(n_q_heads=8, n_kv_heads=2, head_dim=128, dtype=1, kv_dtype=1, max_nodes=8, max_batch=2,
+                                 max_seq_len=64)
+    largest = 3.4028234663852886e38
+    for scale, good in ((1e-40, True), (0.69 * largest, True), (0.7 * largest, False), (largest, False)):
+        cfg.scale = scale                                 # (times log2(e) it has to be finite too)
+        assert (binding.load().sp_probe_tree_workspace_bytes(ctypes.byref(cfg)) > 0) == good, scale
