@@ -116,6 +116,7 @@ def make_rotary(head_dim, rotary_dim=None, base=10000.0, layout="half", scaling=
                                    scaling=_SCALINGS[scaling], base=base, factor=factor,
                                    original_positions=original_positions, beta_fast=beta_fast, beta_slow=beta_slow,
                                    attn_factor=attn_factor)
+    _need(frequencies is None or scaling == "custom", 'frequencies go with scaling="custom" alone')
     if frequencies is not None:
         f = [float(x) for x in frequencies]
         _need(len(f) == dim // 2, f"frequencies must hold {dim // 2} values")

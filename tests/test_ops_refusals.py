@@ -43,3 +43,11 @@ def test_scales_that_fp32_does_not_hold():
     for scale, good in ((1e-40, True), (0.69 * largest, True), (0.7 * largest, False), (largest, False)):
         cfg.scale = scale                                 # (times log2(e) it has to be finite too)
         assert (binding.load().sp_probe_tree_workspace_bytes(ctypes.byref(cfg)) > 0) == good, scale
+
+
+@pytest.mark.parametrize("scaling", ["none", "linear", "ntk", "yarn"])
+def test_frequencies_that_the_scaling_does_not_use(scaling):
+    kw = dict(scaling=scaling, factor=2.0, original_positions=4096)
+    ops.make_rotary(64, **kw)
+    with pytest.raises(ValueError, match="frequencies"):
+        ops.make_rotary(64, frequencies=[0.5] * 32, **kw)
