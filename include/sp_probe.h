@@ -533,6 +533,7 @@ typedef struct sp_tree {
  * and shapes alone, not on the run (no atomics).
  *   seq_lens, block_table  as sp_probe_forward; a block id outside [0, num_blocks) is
  *              read as block 0 (no fault, that sequence's result means nothing)
+ *   store      a head's block (block_size * head_dim elements) has up to 2^31 bytes; more: SP_ERR_UNSUPPORTED
  *   workspace  device, 16-byte aligned, workspace_bytes >= sp_probe_tree_workspace_bytes(cfg),
  *              not initialised; calls that share one must be ordered.  Captured graphs that
  *              may run at the same time need their own

@@ -405,6 +405,8 @@ SP_API int sp_probe_tree_attention(const sp_tree_config* c, const sp_kv_store* s
   if (store->dtype != c->kv_dtype || store->n_kv_heads != c->n_kv_heads || store->head_dim != c->head_dim)
     return SP_ERR_INVALID_ARG;
   if ((int64_t)store->kv.max_blocks_per_seq * store->kv.block_size < (int64_t)c->max_seq_len) return SP_ERR_INVALID_ARG;
+  // places within a head's block are 32-bit byte offsets in the kernels (signed ones on the way)
+  if ((int64_t)store->kv.block_size * c->head_dim * size_of(c->kv_dtype) > (int64_t)1 << 31) return SP_ERR_UNSUPPORTED;
   if (t->n_nodes < 1) return SP_ERR_INVALID_ARG;
   if (t->n_nodes > c->max_nodes || store->kv.batch > c->max_batch) return SP_ERR_CAPACITY;
   if (t->mask && (t->mask_words < (t->n_nodes + 31) / 32 || t->mask_stride < 0 || !aligned(t->mask, 4)))

@@ -8,7 +8,7 @@ import torch
 
 from oracle import cacheops as oracle
 from paper_2608_28099_amd import binding, ops
-from tests.test_gpu_ops import STORES, Tree, make_cache, rotation_error, seeded, tokens, words_of
+from tests.test_gpu_ops import STORES, Tree, make_cache, randn, rotation_error, seeded, tokens, words_of
 
 pytestmark = pytest.mark.gpu
 
@@ -152,3 +152,24 @@ def test_values_that_are_not_finite_under_weights_that_vanish(dev, store, lens, 
     out = ops.tree_attention(c.cache, c.seq_lens, q, k, v, mask=words_of(see).to(dev), max_seq_len=bound or max(lens)).cpu()
     assert not torch.isfinite(out[:, 20:].float()).any()
     assert torch.isfinite(out[:, :7].float()).all() and torch.isfinite(out[:, 8:20].float()).all()
+
+
+@pytest.mark.parametrize("store", STORES)
+@pytest.mark.parametrize("hd", [64, 128])
+def test_the_largest_blocks(dev, store, hd):
+    """A head's block of 2^31 bytes, one per sequence: a token near its end and one in the middle are found."""
+    size = torch.empty(0, dtype=store).element_size()
+    n = (1 << 31) // (hd * size)
+    dtype = torch.float32 if store == torch.float32 else torch.bfloat16
+    cache = ops.PagedCache.allocate(store, 2, 1, hd, n, batch=2, device=dev)
+    pos = torch.tensor([n - 2, n // 2 + 7], dtype=torch.int32, device=dev)
+    seq = torch.tensor([0, 1], dtype=torch.int32, device=dev)
+    x = randn(seeded(hd), 2, 2, hd).to(dtype).to(dev)
+    x[:, 0] = 16.0
+    ops.cache_write(cache, seq, pos, x[:, :1], x[:, 1:])
+    q = torch.full((2, 1, 4, hd), 16.0, dtype=dtype, device=dev)
+    zero = torch.zeros((2, 1, 1, hd), dtype=dtype, device=dev)
+    got = ops.tree_attention(cache, torch.tensor([n - 1, n], dtype=torch.int32, device=dev), q, zero, zero, scale=1.0)
+    value = ops.cache_read(cache, seq, pos, dtype)[1]
+    # scores of 0 and of 16 * 16 * hd >= 16384: the weights of all others vanish
+    assert torch.equal(got, value[:, None].expand(-1, -1, 4, -1))

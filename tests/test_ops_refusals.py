@@ -9,6 +9,7 @@ import pytest
 import torch
 
 from paper_2608_28099_amd import binding, ops
+from tests.test_ops_cpu import P, UNSUPPORTED, rows, store
 
 pytestmark = pytest.mark.skipif(not os.path.exists(binding.LIB_PATH),
                                 reason="libsp_probe.so not built (run __graft_entry__.build())")
@@ -51,3 +52,19 @@ def test_frequencies_that_the_scaling_does_not_use(scaling):
     ops.make_rotary(64, **kw)
     with pytest.raises(ValueError, match="frequencies"):
         ops.make_rotary(64, frequencies=[0.5] * 32, **kw)
+
+
+@pytest.mark.parametrize("dtype,element", [(binding.SP_F32, 4), (binding.SP_BF16, 2), (binding.SP_E4M3, 1)])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_blocks_past_the_offsets_within_them(dtype, element, hd):
+    """A head's block of more than 2^31 bytes; the largest that is taken gets past this check, to one of the workspace."""
+    most = (1 << 31) // (hd * element)
+    cfg = binding.sp_tree_config(n_q_heads=8, n_kv_heads=2, head_dim=hd, dtype=min(dtype, 1), kv_dtype=dtype, max_nodes=8,
+                                 max_batch=2, max_seq_len=64)
+    t = binding.sp_tree(n_nodes=4, q=rows(8), k=rows(2), v=rows(2), out=rows(8))
+    for block, want in ((2 * most, UNSUPPORTED), (4 * most, UNSUPPORTED), (most, -1), (16, -1)):
+        head = block * hd
+        kw = dict(exponent_stride_block=2 * block, exponent_stride_head=block) if element == 1 else {}
+        s = store(dtype, head_dim=hd, block_size=block, k_stride_head=head, v_stride_head=head, k_stride_block=2 * head,
+                  v_stride_block=2 * head, **kw)
+        assert binding.load().sp_probe_tree_attention(ctypes.byref(cfg), ctypes.byref(s), P, P, ctypes.byref(t), P, 0, None) == want
