@@ -524,8 +524,8 @@ typedef struct sp_tree {
  * slots past a sequence's end).  The drafted keys and values are read from k and v and
  * never enter the cache (sp_probe_cache_write puts the accepted ones there).
  * Arithmetic: SP_BF16: products of the stored values (8-bit ones are exact in bf16; with
- * 8-bit keys, query values below 2^-14 of their row's largest, or below 2^-130, are rounded, by
- * 2^-22 of that largest or 2^-136 at most), the softmax's weights rounded to bf16 for the product with the values; fp32 sums,
+ * 8-bit keys, query values below 2^-13 of their row's largest, or below 2^-128, may be rounded, by
+ * 2^-21 of that largest or 2^-136 at most), the softmax's weights rounded to bf16 for the product with the values; fp32 sums,
  * statistics and partial results.  SP_F32: fp32 throughout.  A score (times log2(e)) past fp32's range is an
  * infinity; a row that sees scores of -infinity alone counts as one that sees nothing.  Weights times values are
  * summed before they are divided by the weights' sum, with weights up to 2^8: magnitudes above 2^119 / tokens may

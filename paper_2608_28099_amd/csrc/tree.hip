@@ -232,8 +232,9 @@ struct Wave16 {
 
   // Queries for the products with 8-bit keys: dims 32 la .. + 31 of the row (head dim 64: 16 la .. + 15, of which the
   // second 16 bytes hold ql).  qh: E4M3 with the power of two that brings the row within 448; ql: what is left, times 16.
-  // Eight significant bits of bf16 are four and four, so the two are exact but for values below 2^-14 of the
-  // row's largest, which may be off by 2^-22 of that.
+  // Eight significant bits of bf16 are four and four, so the two are exact down to scaled values of 2^-6.  Smaller ones may
+  // be off by 2^-14, half of E4M3's least step over 16.  The row's largest becomes 224 to 448: that is below 2^-6 / 224 of it, by
+  // 2^-14 / 224 of it at most (of rows within 448 2^-122, where the power ends: below 2^-128, by 2^-136).
   __device__ __forceinline__ void split_queries() {
     u32x4 w[NC];
 #pragma unroll

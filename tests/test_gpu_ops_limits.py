@@ -173,3 +173,32 @@ def test_the_largest_blocks(dev, store, hd):
     value = ops.cache_read(cache, seq, pos, dtype)[1]
     # scores of 0 and of 16 * 16 * hd >= 16384: the weights of all others vanish
     assert torch.equal(got, value[:, None].expand(-1, -1, 4, -1))
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("largest", [1.0, 224.0, 240.0, 255.0, 256.0, 448.0])
+def test_single_query_values_over_8_bit_keys(dev, hd, largest):
+    """One query value alone decides each score (keys of one value): off by 2^-14 / 224 of its row's largest at most, and
+    exact from 2^-6 / 224 of it on."""
+    gen = seeded(int(largest))
+    n = 60
+    q = torch.randint(128, 256, (n,), generator=gen).double() * torch.exp2(-7.0 - torch.arange(n) % 24) * 2.0 ** 8
+    q[0] = 241 * 2.0 ** -14
+    q = torch.where(q > largest, q * 2.0 ** -9, q)
+    cache = make_cache(dev, torch.float8_e4m3fn, (1,), 1, hd, 16, fill=math.nan)
+    kv = torch.zeros((1, 2, hd))
+    kv[:, 0, 9] = 1.0
+    kv[:, 1] = 1.0
+    ids = torch.zeros(1, dtype=torch.int32, device=dev)
+    ops.cache_write(cache, ids, ids, kv[:, :1].to(dev), kv[:, 1:].to(dev))
+    x = torch.zeros((1, n, 1, hd))
+    x[0, :, 0, 9] = q
+    x[0, :, 0, 40] = largest
+    x = x.bfloat16().to(dev)
+    lse = torch.zeros((1, n, 1), device=dev)
+    ops.tree_attention(cache, torch.ones(1, dtype=torch.int32, device=dev), x, x, x, lse=lse, scale=1.0, max_seq_len=1,
+                       mask=torch.zeros((n, 2), dtype=torch.int32, device=dev))
+    off = (lse[0, :, 0].cpu().double() - q).abs()
+    exact = 4 * 2.0 ** -24 * q                            # the factor log2(e), its product, ln(2) and that product
+    assert torch.all(off <= exact + 2.0 ** -14 / 224 * largest), float(off.max())
+    assert torch.all((off <= exact)[q >= 2.0 ** -6 / 224 * largest])
