@@ -357,6 +357,11 @@ def tree_attention(cache: PagedCache, seq_lens, q, k, v, mask=None, counts=None,
 def tree_workspace_bytes(cache: PagedCache, n_q_heads, dtype, nodes, batch=None, max_seq_len=None):
     """Bytes of workspace that tree_attention needs for calls of at most these nodes, with this batch and
     max_seq_len, which plan the launch (0: not supported)."""
+    if dtype not in _ROW_TYPES:
+        raise ValueError("dtype must be float32 or bfloat16")
+    if cache.device.type == "cuda" and _elsewhere(cache.device):  # the launch is planned for its compute units
+        with torch.cuda.device(cache.device):
+            return tree_workspace_bytes(cache, n_q_heads, dtype, nodes, batch, max_seq_len)
     return binding.load().sp_probe_tree_workspace_bytes(
         _tree_config(cache, n_q_heads, dtype, nodes, cache.batch if batch is None else batch,
                      cache.capacity if max_seq_len is None else max_seq_len, 0.0))

@@ -68,3 +68,13 @@ def test_blocks_past_the_offsets_within_them(dtype, element, hd):
         s = store(dtype, head_dim=hd, block_size=block, k_stride_head=head, v_stride_head=head, k_stride_block=2 * head,
                   v_stride_block=2 * head, **kw)
         assert binding.load().sp_probe_tree_attention(ctypes.byref(cfg), ctypes.byref(s), P, P, ctypes.byref(t), P, 0, None) == want
+
+
+def test_workspaces_of_other_types():
+    k = torch.zeros(4, 2, 2048, dtype=torch.bfloat16)
+    cache = ops.PagedCache(k, k, 16, torch.zeros(1, 2, dtype=torch.int32))
+    assert ops.tree_workspace_bytes(cache, 8, torch.bfloat16, 4) > 0
+    assert ops.tree_workspace_bytes(cache, 8, torch.float32, 4) == 0          # of a bf16 cache: not supported
+    for dtype in (torch.float16, torch.float8_e4m3fn, None):
+        with pytest.raises(ValueError):
+            ops.tree_workspace_bytes(cache, 8, dtype, 4)
