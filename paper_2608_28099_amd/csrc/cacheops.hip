@@ -262,8 +262,11 @@ __device__ __forceinline__ void pack(const float (&x)[16], Stored<TS>& out, int&
 // a tile fill an aligned group of 16 bytes' worth of slots (a "group": 4, 8 or 16 rows that
 // follow one another), each dim of it is one 16-byte store; what is left, at a run's
 // ends or with scattered rows, is stored value by value.
-// 49152 rows of 8 heads (bf16 rows, head dim 128): 8-bit 61 us (302 MB, 4.9 TB/s), with a rotation 87 (the angles, and
-// four heads in turn); bf16 94 us (403 MB, 4.3 TB/s), rotated 97.  128 rows: 4.4 to 4.9 us, rotated 8.4 to 9.
+// 49152 rows of 8 heads (bf16 rows, head dim 128) of one sequence from position 0, where every group is whole: 8-bit 61 us
+// (302 MB, 4.9 TB/s), with a rotation 87 (the angles, and four heads in turn); bf16 94 us (403 MB, 4.3 TB/s), rotated 97.
+// Tiles are cut by rows: of a sequence whose first row and slot differ modulo X each tile's end cuts a group, of 8-bit
+// rows a quarter, which goes value by value.  16 sequences of 2K-4K tokens, 44377 rows in all, 8-bit, rotated: 113 us (273 MB, 2.4
+// TB/s).  128 rows: 4.4 to 4.9 us, rotated 8.4 to 9.
 constexpr int kTile = 64;
 
 struct TilePlan {
@@ -455,8 +458,9 @@ __global__ __launch_bounds__(256) void cache_write(const CacheParams p, const sp
 // ---------------------------------------------------------------- read
 // The same tiles the other way, a workgroup per KV head for the keys and one for the values: values
 // through LDS, by groups where the tokens make them, word by word.  49152 rows of 8 heads to bf16
-// (head dim 128): from 8-bit 70 us (302 MB, 4.3 TB/s; byte by byte through LDS 79), from bf16 79 (403 MB,
-// 5.1 TB/s; 82).  Scattered tokens, whose values lie a byte or two apart: 158 and 324.  More heads a workgroup gain
+// (head dim 128) where every group is whole: from 8-bit 70 us (302 MB, 4.3 TB/s; byte by byte through LDS 79), from bf16 79
+// (403 MB, 5.1 TB/s; 82).  32 sequences of 1K-4K 8-bit tokens, 69773 rows in all, a quarter of them outside groups: 121 us (430 MB,
+// 3.5 TB/s).  Scattered tokens, whose values lie a byte or two apart: 158 and 324.  More heads a workgroup gain
 // nothing (8-bit: 71, 76, 77, 88 us with 1, 2, 4, 8).
 template <typename TS>
 __device__ __forceinline__ float value_of(TS x) {

@@ -140,7 +140,9 @@ struct TreePlan {
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-constexpr int kMinSplit = 256;  // tokens
+// Tokens of a split at least (one sequence of 2048, 240 rows of 8 KV heads, which fill a third of the device: 21.5 us; at
+// least 128: 24.3, 192: 23.0, 512: 23.8).
+constexpr int kMinSplit = 256;
 int64_t slots_of(int num_cus) { return (int64_t)num_cus * 3; }  // three workgroups per compute unit, by LDS
 
 // Rows of a wave, and workgroups that the rows of a KV head take.  Workgroups of four waves, 16 or 32 rows each;
@@ -151,7 +153,8 @@ int64_t slots_of(int num_cus) { return (int64_t)num_cus * 3; }  // three workgro
 // A wave of 32 rows reads half as much from LDS per row, but one group of 128 rows in place of two of 64 leaves
 // half as many to spread over the device.  So waves of 32 for bf16 caches (whose waves of 16 are bound by LDS) from 129
 // rows on, where padding to 128 adds at most a fifth and pieces of kMinSplit tokens would still fill the device
-// twice.  Measured (in us, 16 rows a wave / 32): 64 sequences of 6000 tokens: 240 rows 607 / 523, 320 rows 756 / 665,
+// twice.  The bound on the padding is a compromise: of 160 rows a large call would gain by 32 and a small one lose more.
+// Measured (in us, 16 rows a wave / 32): 64 sequences of 6000 tokens: 240 rows 607 / 523, 320 rows 756 / 665,
 // 480 rows 1113 / 937; 160 rows, padded to 192 or 256: 487 / 460; 16 of 4000, 160 rows: 76 / 86, 128 rows: 63 / 77;
 // 240 rows, 4 of 8000: 56.6 / 55.1, one of 2000: 20.2 / 23.6.  8-bit, when keys were converted to bf16, 64 of 6000: 240
 // rows 626 / 652, 320 rows 794 / 873, 480 rows 1189 / 1181; now 577, 727 and 1086 in waves of 16.
@@ -178,12 +181,14 @@ TreePlan tree_plan(const sp_tree_config& c, int nodes, int num_cus) {
   const int64_t n = c.max_seq_len, slots = slots_of(num_cus);
   // As many splits as fill the device once, and pieces of at most an eighth of the longest sequence
   // (or 2048 tokens): a batch of long and short sequences takes several rounds, whose ends level
-  // out (64 sequences of 2K-32K tokens, 320 rows: 1160-1176 us in splits of 4096-8192, 1432 of 1024,
-  // 1383 unsplit; 128 of 1K-8K 8-bit tokens, 64 rows: 208 us in splits of 2048; with keys
-  // converted to bf16 218 so, 236 in splits of 1024, 256 unsplit).
+  // out (64 sequences of 2K-32K tokens, 320 rows: 1208 us in the 8 splits of 4096 that this makes of the longest, 1185 in
+  // 4, 1279 in 16, 1450 in 32, 1457 unsplit).
   // Then up to as many again, until the last round is full: of alike sequences a round that a third of
-  // the device works on costs a whole one (32 of 131072 8-bit tokens, 4 rows: 1435 us in 4 splits
-  // each, 1.33 rounds; 1327 in 8, 2.67; 1362 in 3, one; 2184 unsplit).
+  // the device works on costs a whole one (32 of 131072 8-bit tokens, 4 rows: 1414 us in 4 splits
+  // each, 1.33 rounds; 1328 in 8, 2.67; 1326 in the 9 that this takes, 3; 1363 in 3, one; 2083 unsplit).
+  // The lengths are on the device, so every sequence counts as max_seq_len long here.  Of ragged batches the last round is
+  // not where this looks for it: 128 of 1K-8K 8-bit tokens, 64 rows: 215 us in the 5 splits of 1664 that it takes, 198 in
+  // 4 of 2048, 224 in 8, 249 unsplit.
   const int64_t fill = (n * items + slots - 1) / slots, cap = n / 8 > 2048 ? n / 8 : 2048;
   int64_t len = fill < cap ? fill : cap;
   if (len < kMinSplit) len = kMinSplit;

@@ -144,7 +144,10 @@ __device__ __forceinline__ uint32_t keep_mask(int keep) {
 }
 
 // Eight weights as a bf16 operand.  Rounded to nearest: each moves by at most 2^-8 of itself,
-// what rounding the result to bf16 may cost too.
+// what rounding the result to bf16 may cost too.  So the result is off by 0.0018-0.0023 of itself (root mean square) where weights in
+// fp32 leave 0.0017, its own rounding.  What the rounding leaves as a second operand would give that back for one more
+// product each: 64 sequences of 2K-32K tokens, 320 rows: 1184 -> 1520 us; 128 of 1K-8K 8-bit, 64 rows: 214 -> 276; single tokens of
+// 32 sequences of 131072 8-bit: 1333 -> 1787, of 32768 bf16: 675 -> 679.
 __device__ __forceinline__ bf16x8 weights8(const float* s) {
   bf16x8 w;
 #pragma unroll
@@ -763,12 +766,12 @@ __device__ __forceinline__ float lse_of(float m, float l) {
 // wave (a wave without rows too).  A sequence's last split takes the nodes as well, first, while its
 // first units arrive.  A sequence of one split is finished here, else its splits leave (m, l) and O
 // for tree_merge.
-// What bounds it (8 KV heads, head dim 128).  fp32, the matrix cores: 32 sequences of 8000 tokens, 240 rows: 2060 us, 122
+// What bounds it (8 KV heads, head dim 128).  fp32, the matrix cores: 32 sequences of 8000 tokens, 240 rows: 2090 us, 120
 // TFLOP/s of 157 at the nominal clock; 4 rows, the read: 349 us, 6.0 TB/s.  Few rows, the read: 32 sequences of 131072 8-bit tokens, 4 rows each:
 // 1330 us for 8.7 GB, 6.5 TB/s, where plain reads reach 7.1.  64 rows of 8-bit tokens: vector issue, most of it the
-// values' conversions, one per two values and wave, and the exponentials: 128 sequences of 1K-8K: 208 us, 4.2
-// TB/s and 513 TFLOP/s.  320 rows of bf16: 64 sequences of 2K-32K: 1165 us with their join, 830
-// TFLOP/s (a large library product: 1300), matrix cores 55% busy, three waves per SIMD by registers and LDS; a sixth
+// values' conversions, one per two values and wave, and the exponentials: 128 sequences of 1K-8K: 211 us, 4.2
+// TB/s and 506 TFLOP/s.  320 rows of bf16: 64 sequences of 2K-32K: 1185-1230 us with their join, 780-810
+// TFLOP/s (a large library product: 1300), matrix cores 53% busy, three waves per SIMD by registers and LDS; a sixth
 // of its wave slots have no rows (320 in groups of 128).  One sequence of 2048, 240 rows: 20 us, a chain of loads.
 constexpr int kWaves = 4;
 
